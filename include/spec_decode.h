@@ -280,6 +280,8 @@ int spec_uniforms(uint64_t seed, const int32_t* positions, const int32_t* sequen
 enum { SPEC_ARCH_GPT = 0, SPEC_ARCH_LLAMA = 1, SPEC_ARCH_T5 = 2, SPEC_ARCH_BIGRAM = 3, SPEC_ARCH_COPY = 4 };
 enum { SPEC_FFN_GELU = 0, SPEC_FFN_GATED_GELU = 1, SPEC_FFN_SWIGLU = 2 };
 enum { SPEC_DTYPE_FP32 = 0, SPEC_DTYPE_BF16 = 1, SPEC_DTYPE_FP16 = 2 /* cached K,V rows only */ };
+/* Eight-bit rows with scales; the operators at the end of this file take them (and fp16 for other tensors too), models do not. */
+enum { SPEC_DTYPE_E4M3 = 3, SPEC_DTYPE_INT8 = 4 };
 
 typedef struct spec_model_cfg {
     int arch;             /* SPEC_ARCH_* */
@@ -631,6 +633,116 @@ int spec_device_error(void);
  * the model's one-row passes are a chain of kernels. */
 int spec_timeout_drill_pass(spec_ctx* ctx, int which);
 int spec_timeout_drill(void* stream);
+
+/* ------------------------------------------------------------------------- *
+ * Operators of a verification pass for callers with models of their own (the
+ * paper takes M_p and M_q as given, Section 2.1, and asks of the target one pass
+ * over gamma + 1 rows, which is bound by the bytes of weights and cached rows,
+ * Section 3.4): a decoder block with 8-bit weights, activations and K,V rows is
+ *   spec_norm_fp8 -> spec_linear_fp8 (q, k, v) -> spec_kv_append ->
+ *   spec_paged_attention -> spec_quantize_fp8 -> spec_linear_fp8 (+ residual) ->
+ *   spec_norm_fp8 -> spec_linear_fp8 (gated) -> spec_quantize_fp8 ->
+ *   spec_linear_fp8 (+ residual).
+ * All pointers are DEVICE pointers, tensors are row-major and dense unless a
+ * stride is given, calls are asynchronous on `stream`, allocate nothing and can
+ * be captured into a graph.  Outputs must not overlap inputs except where it is
+ * said.  A result depends on the call's inputs alone: no atomics, sums in a fixed
+ * order, the same bits every time.  rows == 0 or batch == 0 is a no-op.
+ *
+ * A row y in 8 bits is codes c and one fp32 scale s, value c * s: with a the
+ * largest |y|, s = 1 if a == 0, else a * fl(1 / 448) (e4m3) or a * fl(1 / 127) (int8), at
+ * least 2^-80; c = y * (1 / s) rounded to nearest, ties to even.  A row with a NaN or
+ * an infinity has a scale that is not finite and reads back as NaN.
+ *
+ * spec_quantize_fp8: x [rows, d] fp32, bf16 or fp16 (x_dtype) to e4m3 codes
+ *   [rows, d] and scales [rows]; 1 <= d <= 32768.  Also makes the weights of
+ *   spec_linear_fp8 (a scale per row of W).
+ *
+ * spec_norm_fp8: h = x + residual, rounded to h_dtype (fp32 or x's) where it is
+ *   stored; y = (h * gain) * (mean(h^2) + eps)^(-1/2) over the row; codes and
+ *   scales of y.  residual [rows, d] and h [rows, d] have type h_dtype; residual
+ *   NULL: h = x; h NULL: the sum is not stored (and not rounded).  h may be
+ *   residual, or x where the types are the same.  gain [d] fp32, eps > 0.
+ *
+ * spec_linear_fp8: x [rows, k] and w [n_w, k] e4m3 codes with x_scales [rows] and
+ *   w_scales [n_w], k a multiple of 16, codes 16-byte aligned:
+ *     z[r][n] = x_scales[r] * w_scales[n] * sum_k x[r][k] w[n][k] (+ bias[n]),
+ *     y[r][n] = act(z[r][n]) (+ residual[r][n]),
+ *   act: SPEC_ACT_NONE, SPEC_ACT_GELU (tanh approximation), SPEC_ACT_SILU with
+ *   n_w = n_out; SPEC_ACT_GATED_GELU, SPEC_ACT_SWIGLU with n_w = 2 n_out, rows
+ *   0..n_out-1 the gate g, the others the up projection u, act = gelu(g) u or
+ *   silu(g) u.  bias [n_w] fp32 or NULL; residual [rows, n_out] of y's type or
+ *   NULL, may be y; y [rows, n_out] fp32, bf16 or fp16 (y_dtype).  Sums are fp32.
+ *   Runs on the tensor cores; gives up on an expired wait as the GEMMs above do
+ *   (spec_device_error).
+ *
+ * Paged K,V rows: pool [pages][K, V][n_kv_heads][page_size][d_head] in kv_dtype
+ * (SPEC_DTYPE_FP16, BF16, E4M3 or INT8), 16-byte aligned, and for the two 8-bit
+ * types scales [pages][K, V][n_kv_heads][page_size] fp32 (a scale per token and
+ * head; those of rows that are read have to be above zero).  page_size: a power
+ * of two from 32 to 256; d_head 64 or 128.  page_table [batch][max_pages] int32:
+ * the page of each page_size positions of a sequence.  An entry outside [0, pages)
+ * is not followed: rows there are neither written nor read back, and attention
+ * goes on as if the keys there did not exist.  Pages may be shared for reading;
+ * two rows written to one place in one call, or by calls that may overlap, race.
+ *
+ * spec_kv_append: row i of sequence b (k, v [batch, rows, n_kv_heads, d_head] of
+ *   `dtype`, one row k_stride / v_stride ELEMENTS behind the last, heads dense)
+ *   goes to position start[b] + i, for i < counts[b] (counts NULL: all rows);
+ *   rows beyond, negative starts and positions past the table are left out.  rope
+ *   (may be NULL) [rope_positions][d_head / 2][2] fp32, (cos, sin) of position *
+ *   frequency j, rotates K's pairs (j, j + d_head / 2) first: x cos - y sin,
+ *   y cos + x sin; positions past the table are left out.  q (may be NULL,
+ *   with q_out) [batch, rows, n_heads, d_head] of `dtype` with q_stride gets the
+ *   same rotation, rounded into q_out (dense; may be q if that is dense); rows
+ *   that are left out are not touched.  fp16 pools hold +-65504 for what is beyond.
+ *
+ * spec_kv_read: the rows that an append with the same start, counts and rows has
+ *   written, into k and v [batch, rows, n_kv_heads, d_head] of `dtype`; rows that
+ *   are left out are not touched.
+ *
+ * spec_paged_attention: lengths [batch] counts the cached tokens of a sequence
+ *   with the `rows` new ones; row i stands at position p = lengths[b] - rows + i
+ *   and sees the keys 0..p:
+ *     out = sum_j softmax_j(scale * q . k_j) v_j,
+ *   zeros for a row that sees no key (p < 0, or no page).  q [batch, rows, n_heads,
+ *   d_head] bf16 or fp16 with q_stride ELEMENTS between rows (a multiple of 4; q
+ *   and out 8-byte aligned), out dense and of the same type; query head h reads
+ *   KV head h / (n_heads / n_kv_heads).  A 16-bit pool has q's type, an 8-bit one
+ *   goes with either.  Lengths past the table's capacity: keys beyond do not
+ *   exist.  Queries are multiplied in fp16 after a power of two per row (bf16
+ *   pools: as they are), weights are rounded to 16 bits for the second product,
+ *   all sums are fp32.  workspace: spec_paged_attention_workspace_bytes() bytes,
+ *   256-byte aligned, contents arbitrary, not shared by calls that may overlap.
+ *
+ * Errors: SPEC_ERR_BAD_ARG for null pointers, sizes, types, alignments or strides
+ * other than described (nothing is launched then); SPEC_ERR_CUDA if a launch fails.
+ * ------------------------------------------------------------------------- */
+enum { SPEC_ACT_NONE = 0, SPEC_ACT_GELU = 1, SPEC_ACT_SILU = 2, SPEC_ACT_GATED_GELU = 3, SPEC_ACT_SWIGLU = 4 };
+
+int spec_quantize_fp8(const void* x, int x_dtype, int rows, int d, void* codes, float* scales, void* stream);
+
+int spec_norm_fp8(const void* x, int x_dtype, const void* residual, void* h, int h_dtype, const float* gain, float eps,
+                  int rows, int d, void* codes, float* scales, void* stream);
+
+int spec_linear_fp8(const void* x, const float* x_scales, const void* w, const float* w_scales, const float* bias, int act,
+                    const void* residual, void* y, int y_dtype, int rows, int n_out, int k, void* stream);
+
+int spec_kv_append(const void* q, const void* k, const void* v, int dtype, int64_t q_stride, int64_t k_stride,
+                   int64_t v_stride, int n_heads, int n_kv_heads, int d_head, int batch, int rows, const int32_t* start,
+                   const int32_t* counts, const float* rope, int rope_positions, void* q_out, void* pool, float* scales,
+                   int kv_dtype, int pages, int page_size, const int32_t* page_table, int max_pages, void* stream);
+
+int spec_kv_read(const void* pool, const float* scales, int kv_dtype, int pages, int page_size, int n_kv_heads, int d_head,
+                 const int32_t* page_table, int max_pages, int batch, int rows, const int32_t* start,
+                 const int32_t* counts, void* k, void* v, int dtype, void* stream);
+
+size_t spec_paged_attention_workspace_bytes(int batch, int rows, int n_heads, int n_kv_heads, int d_head);
+
+int spec_paged_attention(const void* q, int dtype, int64_t q_stride, const void* pool, const float* scales, int kv_dtype,
+                         int pages, int page_size, const int32_t* page_table, int max_pages, const int32_t* lengths,
+                         int batch, int rows, int n_heads, int n_kv_heads, int d_head, float scale, void* out,
+                         void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

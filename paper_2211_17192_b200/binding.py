@@ -99,6 +99,21 @@ def _declare(h):
     h.spec_pack_weight.argtypes = [vp, i32, i32, vp, vp]
     h.spec_device_error.restype = i32
     h.spec_device_error.argtypes = []
+    i64 = c.c_int64
+    h.spec_quantize_fp8.restype = i32
+    h.spec_quantize_fp8.argtypes = [vp, i32, i32, i32, vp, vp, vp]
+    h.spec_norm_fp8.restype = i32
+    h.spec_norm_fp8.argtypes = [vp, i32, vp, vp, i32, vp, f32, i32, i32, vp, vp, vp]
+    h.spec_linear_fp8.restype = i32
+    h.spec_linear_fp8.argtypes = [vp, vp, vp, vp, vp, i32, vp, vp, i32, i32, i32, i32, vp]
+    h.spec_kv_append.restype = i32
+    h.spec_kv_append.argtypes = [vp, vp, vp, i32, i64, i64, i64, i32, i32, i32, i32, i32, vp, vp, vp, i32, vp, vp, vp, i32, i32, i32, vp, i32, vp]
+    h.spec_kv_read.restype = i32
+    h.spec_kv_read.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, i32, i32, i32, vp, vp, vp, vp, i32, vp]
+    h.spec_paged_attention_workspace_bytes.restype = sz
+    h.spec_paged_attention_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+    h.spec_paged_attention.restype = i32
+    h.spec_paged_attention.argtypes = [vp, i32, i64, vp, vp, i32, i32, i32, vp, i32, vp, i32, i32, i32, i32, i32, f32, vp, vp, sz, vp]
 
 
 def _check(status):
@@ -323,6 +338,187 @@ def spec_linear_partials(x, w_packed, n_out, workspace, split_input=True, rows=N
 
 def spec_device_error():
     return int(lib().spec_device_error())
+
+
+# --------------------------------------------------------------------------- #
+# operators of a verification pass in 8 bits, for callers with models of their own
+# --------------------------------------------------------------------------- #
+ACTIVATIONS = {"none": 0, "gelu": 1, "silu": 2, "gated_gelu": 3, "swiglu": 4}
+_DTYPE_CODES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3, torch.int8: 4}
+_FLOATS = (torch.float32, torch.bfloat16, torch.float16)
+
+
+def _need(ok, message):
+    if not ok:
+        raise ValueError(message)
+
+
+def _operand(t, name, dtypes, shape=None, contiguous=True):
+    """The address of a tensor that has been looked at: on the current GPU, of one of the types, of the shape."""
+    _need(isinstance(t, torch.Tensor) and t.is_cuda, f"{name} must be a CUDA tensor")
+    _need(t.device.index == torch.cuda.current_device(), f"{name} is on {t.device}, not on the current device")
+    _need(t.dtype in dtypes, f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
+    _need(shape is None or tuple(t.shape) == tuple(shape), f"{name} must be {list(shape) if shape is not None else ''}, got {list(t.shape)}")
+    _need(not contiguous or t.is_contiguous(), f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _optional(t, name, dtypes, shape=None):
+    return None if t is None else _operand(t, name, dtypes, shape)
+
+
+def _rows_of_heads(t, name, dtypes, shape=None):
+    """Address and row stride of [B, rows, heads, d_head] with dense heads: a whole tensor or a part of a fused projection's output."""
+    _need(isinstance(t, torch.Tensor) and t.dim() == 4, f"{name} must be [B, rows, heads, d_head]")
+    where = _operand(t, name, dtypes, shape, contiguous=False)
+    batch, rows, heads, d = t.shape
+    s = t.stride()
+    _need(t.numel() == 0 or ((d == 1 or s[3] == 1) and (heads == 1 or s[2] == d)), f"{name}: the heads of a row must lie behind one another")
+    stride = s[1] if rows > 1 else s[0] if batch > 1 else heads * d
+    _need(t.numel() == 0 or batch == 1 or rows == 1 or s[0] == rows * s[1], f"{name}: one row stride for all rows")
+    return where, stride
+
+
+def _pool_args(pool, scales, page_table, batch):
+    _need(isinstance(pool, torch.Tensor) and pool.dim() == 5 and pool.shape[1] == 2, "pool must be [pages, 2, kv heads, page size, d_head]")
+    kinds = (torch.float16, torch.bfloat16, torch.float8_e4m3fn, torch.int8)
+    where = _operand(pool, "pool", kinds)
+    eight = pool.dtype in kinds[2:]
+    _need(eight or scales is None, "scales go with an 8-bit pool")
+    at = _operand(scales, "scales", (torch.float32,), pool.shape[:4]) if eight else None
+    _need(isinstance(page_table, torch.Tensor) and page_table.dim() == 2 and page_table.shape[0] == batch, "page_table must be [B, max_pages]")
+    table = _operand(page_table, "page_table", (torch.int32,))
+    pages, _, heads, page_size, d = pool.shape
+    return where, at, _DTYPE_CODES[pool.dtype], pages, page_size, table, page_table.shape[1], heads, d
+
+
+def spec_quantize_fp8(x, codes=None, scales=None):
+    """Rows in e4m3 with a scale each: x [rows, d] fp32, bf16 or fp16 CUDA -> (codes [rows, d] float8_e4m3fn, scales [rows] fp32),
+    value = code * scale.  Also how the weights of `spec_linear_fp8` are made."""
+    _need(isinstance(x, torch.Tensor) and x.dim() == 2, "x must be [rows, d]")
+    where = _operand(x, "x", _FLOATS)
+    rows, d = x.shape
+    codes = torch.empty((rows, d), dtype=torch.float8_e4m3fn, device=x.device) if codes is None else codes
+    scales = torch.empty(rows, dtype=torch.float32, device=x.device) if scales is None else scales
+    _check(lib().spec_quantize_fp8(where, _DTYPE_CODES[x.dtype], rows, d, _operand(codes, "codes", (torch.float8_e4m3fn,), (rows, d)),
+                                   _operand(scales, "scales", (torch.float32,), (rows,)), _stream()))
+    return codes, scales
+
+
+def spec_norm_fp8(x, gain, eps=1e-6, residual=None, h=None, codes=None, scales=None):
+    """Residual addition, RMS norm and an 8-bit output: h = x + residual (x where residual is None), codes and scales of
+    rmsnorm(h) * gain; x [rows, d] fp32, bf16 or fp16, gain [d] fp32, residual and h [rows, d] fp32 or of x's type.
+    Returns (codes, scales, h); h is allocated when a residual is given without it, may be the residual itself, and is
+    None when neither is given."""
+    _need(isinstance(x, torch.Tensor) and x.dim() == 2, "x must be [rows, d]")
+    where = _operand(x, "x", _FLOATS)
+    rows, d = x.shape
+    kinds = (torch.float32, x.dtype)
+    if residual is not None:
+        _operand(residual, "residual", kinds, (rows, d))
+        h = torch.empty_like(residual) if h is None else h
+    if h is not None:
+        _operand(h, "h", kinds if residual is None else (residual.dtype,), (rows, d))
+    codes = torch.empty((rows, d), dtype=torch.float8_e4m3fn, device=x.device) if codes is None else codes
+    scales = torch.empty(rows, dtype=torch.float32, device=x.device) if scales is None else scales
+    _check(lib().spec_norm_fp8(where, _DTYPE_CODES[x.dtype], None if residual is None else residual.data_ptr(), None if h is None else h.data_ptr(),
+                               0 if h is None else _DTYPE_CODES[h.dtype], _operand(gain, "gain", (torch.float32,), (d,)), float(eps), rows, d,
+                               _operand(codes, "codes", (torch.float8_e4m3fn,), (rows, d)), _operand(scales, "scales", (torch.float32,), (rows,)),
+                               _stream()))
+    return codes, scales, h
+
+
+def spec_linear_fp8(x, x_scales, w, w_scales, bias=None, act="none", residual=None, y=None, dtype=torch.float32):
+    """y = act(x . W^T * scales + bias) + residual on the tensor cores: x [rows, k] and w [n_w, k] float8_e4m3fn with
+    x_scales [rows] and w_scales [n_w]; act "none", "gelu", "silu" (n_out = n_w), "gated_gelu" or "swiglu" (n_out = n_w / 2, gate
+    rows first); bias [n_w] fp32; residual and y [rows, n_out] of one type, y is allocated in the residual's type or `dtype`
+    when not given and may be the residual."""
+    _need(act in ACTIVATIONS, f"act must be one of {', '.join(ACTIVATIONS)}")
+    _need(isinstance(x, torch.Tensor) and x.dim() == 2 and isinstance(w, torch.Tensor) and w.dim() == 2 and x.shape[1] == w.shape[1],
+          "x must be [rows, k] and w [n_w, k]")
+    (rows, k), n_w = x.shape, w.shape[0]
+    gated = act in ("gated_gelu", "swiglu")
+    _need(not gated or n_w % 2 == 0, "a gated activation takes two halves of w")
+    n_out = n_w // 2 if gated else n_w
+    where = _operand(x, "x", (torch.float8_e4m3fn,))
+    if y is None:
+        y = torch.empty((rows, n_out), dtype=dtype if residual is None else residual.dtype, device=x.device)
+    out = _operand(y, "y", _FLOATS, (rows, n_out))
+    _check(lib().spec_linear_fp8(where, _operand(x_scales, "x_scales", (torch.float32,), (rows,)), _operand(w, "w", (torch.float8_e4m3fn,)),
+                                 _operand(w_scales, "w_scales", (torch.float32,), (n_w,)), _optional(bias, "bias", (torch.float32,), (n_w,)),
+                                 ACTIVATIONS[act], _optional(residual, "residual", (y.dtype,), (rows, n_out)), out, _DTYPE_CODES[y.dtype],
+                                 rows, n_out, k, _stream()))
+    return y
+
+
+def spec_kv_append(k, v, pool, scales, page_table, start, counts=None, rope=None, q=None, q_out=None):
+    """New tokens' K and V into a paged cache, quantised as they are written where the pool is float8_e4m3fn or int8, K (and q)
+    rotated first when `rope` [positions, d_head / 2, 2] (cos, sin) is given.  k, v (and q) [B, rows, heads, d_head] fp32,
+    bf16 or fp16, parts of one projection's output or tensors of their own; pool [pages, 2, kv heads, page size, d_head];
+    scales [pages, 2, kv heads, page size] fp32 for 8-bit pools, else None; page_table [B, max_pages], start [B],
+    counts [B] int32.  Row i of sequence b goes to position start[b] + i if i < counts[b].  Returns q_out (None without q)."""
+    _need(isinstance(k, torch.Tensor) and k.dim() == 4, "k must be [B, rows, heads, d_head]")
+    batch, rows, n_kv, d = k.shape
+    where, at, kv_dtype, pages, page_size, table, width, pool_heads, pool_d = _pool_args(pool, scales, page_table, batch)
+    _need((n_kv, d) == (pool_heads, pool_d), "k and the pool differ in heads or d_head")
+    k_at, k_stride = _rows_of_heads(k, "k", _FLOATS)
+    v_at, v_stride = _rows_of_heads(v, "v", (k.dtype,), k.shape)
+    n_heads, q_at, q_stride, out = 0, None, 0, None
+    if q is not None:
+        _need(q.dim() == 4 and q.shape[0] == batch and q.shape[1] == rows and q.shape[3] == d, "q must be [B, rows, heads, d_head]")
+        n_heads = q.shape[2]
+        q_at, q_stride = _rows_of_heads(q, "q", (k.dtype,))
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+        out = _operand(q_out, "q_out", (q.dtype,), q.shape)
+    else:
+        _need(q_out is None, "q_out goes with q")
+    if rope is not None:
+        _need(rope.dim() == 3 and tuple(rope.shape[1:]) == (d // 2, 2), "rope must be [positions, d_head / 2, 2]")
+    _check(lib().spec_kv_append(q_at, k_at, v_at, _DTYPE_CODES[k.dtype], q_stride, k_stride, v_stride, n_heads, n_kv, d, batch, rows,
+                                _operand(start, "start", (torch.int32,), (batch,)), _optional(counts, "counts", (torch.int32,), (batch,)),
+                                _optional(rope, "rope", (torch.float32,)), 0 if rope is None else rope.shape[0], out, where, at, kv_dtype, pages,
+                                page_size, table, width, _stream()))
+    return q_out
+
+
+def spec_kv_read(pool, scales, page_table, start, rows, counts=None, dtype=torch.float32, k=None, v=None):
+    """The cached rows at start[b] .. start[b] + counts[b] - 1 (`rows` of them without counts) of every sequence, widened:
+    (k, v) [B, rows, kv heads, d_head] of `dtype`, zeros where there is no row, or into the tensors given, whose other rows
+    stay as they are."""
+    _need(isinstance(page_table, torch.Tensor) and page_table.dim() == 2, "page_table must be [B, max_pages]")
+    batch = page_table.shape[0]
+    where, at, kv_dtype, pages, page_size, table, width, n_kv, d = _pool_args(pool, scales, page_table, batch)
+    shape = (batch, rows, n_kv, d)
+    k = torch.zeros(shape, dtype=dtype, device=pool.device) if k is None else k
+    v = torch.zeros(shape, dtype=k.dtype, device=pool.device) if v is None else v
+    k_at, v_at = _operand(k, "k", _FLOATS, shape), _operand(v, "v", (k.dtype,), shape)
+    _check(lib().spec_kv_read(where, at, kv_dtype, pages, page_size, n_kv, d, table, width, batch, rows, _operand(start, "start", (torch.int32,), (batch,)),
+                              _optional(counts, "counts", (torch.int32,), (batch,)), k_at, v_at, _DTYPE_CODES[k.dtype], _stream()))
+    return k, v
+
+
+def spec_paged_attention_workspace_bytes(batch, rows, n_heads, n_kv_heads, d_head):
+    return int(lib().spec_paged_attention_workspace_bytes(batch, rows, n_heads, n_kv_heads, d_head))
+
+
+def spec_paged_attention(q, pool, scales, page_table, lengths, scale=None, out=None, workspace=None):
+    """Attention of every sequence's last `rows` tokens over its cached rows (their own among them): q [B, rows, heads, d_head]
+    bf16 or fp16, the cache as in `spec_kv_append`, lengths [B] int32 the tokens cached with the new ones; row i sees the keys at
+    and before position lengths[b] - rows + i.  scale defaults to d_head ** -0.5.  Returns out, of q's shape and type; it and
+    the workspace are allocated when not given."""
+    _need(isinstance(q, torch.Tensor) and q.dim() == 4, "q must be [B, rows, heads, d_head]")
+    batch, rows, heads, d = q.shape
+    where, at, kv_dtype, pages, page_size, table, width, n_kv, pool_d = _pool_args(pool, scales, page_table, batch)
+    _need(d == pool_d and heads % n_kv == 0, "q and the pool differ in d_head, or its heads are no multiple of the pool's")
+    q_at, q_stride = _rows_of_heads(q, "q", (torch.bfloat16, torch.float16))
+    out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+    if workspace is None:
+        workspace = torch.empty(spec_paged_attention_workspace_bytes(batch, rows, heads, n_kv, d), dtype=torch.uint8, device=q.device)
+    _check(lib().spec_paged_attention(q_at, _DTYPE_CODES[q.dtype], q_stride, where, at, kv_dtype, pages, page_size, table, width,
+                                      _operand(lengths, "lengths", (torch.int32,), (batch,)), batch, rows, heads, n_kv, d,
+                                      d ** -0.5 if scale is None else float(scale), _operand(out, "out", (q.dtype,), q.shape),
+                                      _operand(workspace, "workspace", (torch.uint8,)), workspace.numel(), _stream()))
+    return out
 
 
 # --------------------------------------------------------------------------- #

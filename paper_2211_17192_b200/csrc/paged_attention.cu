@@ -1,0 +1,740 @@
+// Attention of the few new tokens of every sequence (one, or the gamma + 1 rows of a verification pass) over its paged K,V rows:
+//   S_j = scale * q . k_j for the keys j at or before the row's position,  o = sum_j softmax(S)_j v_j.
+//
+// Bound by the cached rows' bytes: they are read once for all queries of a KV head, as they lie (8 bits or 16), and widened in
+// registers on their way into mma.sync (M = 16 queries, fp16 or, for bf16 caches, bf16; sums fp32).  Scales of 8-bit rows stay
+// outside the products: with k_j = sk_j kc_j and v_j = sv_j vc_j,
+//   S_j = (scale sk_j)(q . kc_j),   o = sum_j w_j vc_j / sum_j w_j / sv_j   with w_j = exp(S_j) sv_j = 2^(S_j log2 e + log2 sv_j):
+// the running maximum is taken of the latter exponent, so that w_j, which is rounded to fp16 for the second product, is at most
+// about 1 whatever the scales are, and one exponential per score serves both sums.
+//
+// Work: tiles of 64 keys of a segment (sequence, block of queries, KV head).  The lengths are known on the device only, so every
+// CTA adds them up and takes an equal, contiguous run of all tiles (the longest sequence does not decide, whatever the capacity of
+// the page table); a segment that several CTAs share leaves (maximum, sum, weighted rows) per CTA in the workspace, and a second
+// kernel joins them in order.  No atomics: the same bits every time.
+//
+// A CTA has four groups of warps; a group takes 16 of a tile's 64 keys, a warp of it 16 queries.  Tiles come through a ring of
+// cp.async stages; rows that are not there (past the limit, or on a page outside the pool) are filled with zeros and masked.
+#include <algorithm>
+
+#include "paged.cuh"
+
+namespace spec {
+namespace {
+
+constexpr int kTileKeys = 64;
+constexpr int kGroups = 4;       // warps along a tile's keys, 16 keys each
+constexpr int kMostCtas = 592;   // 148 SMs x 4
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kSlack = 8.0f;   // the running maximum may lag by this: w <= 2^8 stays in fp16's range
+
+struct AttnArgs {
+    Paged cache;
+    const void* pool;
+    const float* scales;
+    const void* q;
+    void* out;
+    const int32_t* lengths;
+    float* partial;    // [slots][queries of a block][D]
+    float2* partial_ml;  // [slots][queries of a block]: maximum, sum
+    long long q_stride;
+    float scale;
+    int batch, rows, n_heads, group, blocks, units;  // blocks: of queries per (sequence, KV head); units = batch * blocks
+    int q_bf16, grid;
+};
+
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t to, const void* from, bool there) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(there ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ uint32_t shared_u32(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+
+template <bool BF16>
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint4& a, uint32_t b0, uint32_t b1) {
+    if constexpr (BF16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack2(float x, float y) {
+    if constexpr (BF16) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    } else {
+        const __half2 v = __floats2half2_rn(x, y);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    }
+}
+// Bytes 2 i and 2 i + 1 (STEP 1) of four codes, or bytes i and i + 2 (STEP 2), as two fp16 values.
+template <int KV, int STEP>
+__device__ __forceinline__ void widen(uint32_t codes, uint32_t& first, uint32_t& second) {
+    if constexpr (KV == SPEC_DTYPE_INT8) {
+        // code + 128 as the low bits of 1024.0, minus 1152: exact
+        const uint32_t biased = codes ^ 0x80808080u;
+        const uint32_t x = __byte_perm(biased, 0x64646464u, STEP == 1 ? 0x4140 : 0x4240), y = __byte_perm(biased, 0x64646464u, STEP == 1 ? 0x4342 : 0x4341);
+        const __half2 off = __floats2half2_rn(1152.0f, 1152.0f);
+        const __half2 a = __hsub2(*reinterpret_cast<const __half2*>(&x), off), b = __hsub2(*reinterpret_cast<const __half2*>(&y), off);
+        first = *reinterpret_cast<const uint32_t*>(&a);
+        second = *reinterpret_cast<const uint32_t*>(&b);
+    } else {
+        if constexpr (STEP == 2) codes = __byte_perm(codes, 0u, 0x3120);
+        asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\tcvt.rn.f16x2.e4m3x2 %1, hi;\n\t}" : "=r"(first), "=r"(second) : "r"(codes));
+    }
+}
+
+// Whether a NaN or an infinity is among 16 bytes of a row.
+template <int KV>
+__device__ __forceinline__ bool not_numbers(const uint4& v) {
+    const uint32_t words[4] = {v.x, v.y, v.z, v.w};
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (KV == SPEC_DTYPE_E4M3) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) any |= (words[i] >> (8 * j) & 0x7fu) == 0x7fu;
+        } else {
+            constexpr uint32_t exponent = KV == SPEC_DTYPE_BF16 ? 0x7f80u : 0x7c00u;
+            any |= (words[i] & exponent) == exponent || (words[i] >> 16 & exponent) == exponent;
+        }
+    }
+    return any;
+}
+
+// One segment of a CTA's run of tiles.
+struct Segment {
+    int unit, head, tile0, tile1, tiles, limit;  // limit: keys before it exist for some row of the block
+};
+
+// Tiles of a unit (sequence, block of queries): the keys up to the position of the block's last row.
+template <int QT>
+__device__ __forceinline__ int unit_limit(const AttnArgs& a, int unit) {
+    const int b = unit / a.blocks, block = unit - b * a.blocks;
+    const long long capacity = static_cast<long long>(a.cache.width) << a.cache.page_shift;
+    const int length = a.lengths[b];
+    const int last_row = min(a.rows - 1, (block * QT + QT - 1) / a.group);
+    const long long limit = static_cast<long long>(length) - a.rows + last_row + 1;
+    return static_cast<int>(max(0ll, min(min(limit, static_cast<long long>(length)), capacity)));
+}
+
+// The unit in which tile `wanted` of all lies, with the tiles (of one KV head) before it; and the sum over all units.
+// `wanted(total)` is called once the sum is known.  All threads of the block; `scratch`: 40 long longs.
+template <int QT, typename F>
+__device__ __forceinline__ void find_unit(const AttnArgs& a, long long* scratch, F wanted, long long& total, int& unit, long long& before) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    long long base = 0, target = 0;
+    unit = -1;
+    for (int round = a.units > static_cast<int>(blockDim.x) ? 0 : 1; round < 2; ++round) {  // (more units than threads: add up first, look then)
+        if (round == 1 && a.units > static_cast<int>(blockDim.x)) {
+            total = base * a.cache.n_kv;
+            target = wanted(total);
+            base = 0;
+        }
+        for (int u0 = 0; u0 < a.units; u0 += blockDim.x) {
+            const int u = u0 + threadIdx.x;
+            const long long mine = u < a.units ? (unit_limit<QT>(a, u) + kTileKeys - 1) / kTileKeys : 0;
+            long long upto = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long up = __shfl_up_sync(kFullMask, upto, o);
+                if (lane >= o) upto += up;
+            }
+            __syncthreads();  // (scratch is free)
+            if (lane == 31) scratch[warp] = upto;
+            __syncthreads();
+            long long all = 0, front = 0;
+            for (int w = 0; w < warps; ++w) {
+                if (w < warp) front += scratch[w];
+                all += scratch[w];
+            }
+            upto += base + front;
+            if (round == 1) {
+                if (a.units <= static_cast<int>(blockDim.x)) {
+                    total = all * a.cache.n_kv;
+                    target = wanted(total);
+                }
+                if ((upto - mine) * a.cache.n_kv <= target && target < upto * a.cache.n_kv) {
+                    scratch[32] = u;
+                    scratch[33] = upto - mine;
+                }
+            }
+            base += all;
+        }
+    }
+    if (total == 0 || target >= total) return;
+    __syncthreads();
+    unit = static_cast<int>(scratch[32]);
+    before = scratch[33];
+}
+
+__device__ __forceinline__ long long first_tile(long long total, int cta, int ctas) { return total * cta / ctas; }
+__device__ __forceinline__ int owner_of(long long total, long long tile, int ctas) { return static_cast<int>(((tile + 1) * ctas - 1) / total); }
+__device__ __forceinline__ int ctas_of(long long total, int grid) { return static_cast<int>(min(total, static_cast<long long>(grid))); }
+
+template <int D, int KV, int MT>
+struct Shape {
+    static constexpr bool kEight = KV == SPEC_DTYPE_E4M3 || KV == SPEC_DTYPE_INT8;
+    static constexpr bool kBf16 = KV == SPEC_DTYPE_BF16;
+    static constexpr int kRowBytes = D * (kEight ? 1 : 2);
+    static constexpr int kChunks = kRowBytes / 16;
+    static constexpr int kQueries = 16 * MT;
+    static constexpr int kThreads = 32 * kGroups * MT;
+    static constexpr int kStageBytes = 2 * kTileKeys * kRowBytes + 2 * kTileKeys * 4;
+    static constexpr int kStages = 3;
+    static constexpr int kQueryBytes = kQueries * D * 2;
+    static constexpr int kMerge = 2 * MT * 16 * (D + 2) * 4;  // two groups' states
+    static constexpr int kRing = kStages * kStageBytes > kMerge ? kStages * kStageBytes : kMerge;
+    static constexpr int kSmem = kRing + kQueryBytes + kQueries * 4 + 40 * 8 + kGroups * MT * 16 * 16 + kTileKeys * 4;
+    // Place of 16-byte chunk c of row r: rows whose chunks meet in the reads below lie in different banks.
+    static __device__ __forceinline__ int place(int r, int c) { return r * kRowBytes + ((kRowBytes == 64 ? c ^ ((r >> 1) & 3) : c ^ (r & 7)) << 4); }
+    // Which of eight keys a lane quad n reads, and column n of a score tile stands for: neighbours differ in the bit that moves a
+    // row's chunks to the other half of the banks.
+    static __device__ __forceinline__ int key_of(int n) { return kRowBytes == 64 ? n : (n & 1) * 4 + (n >> 1); }
+};
+
+template <int D, int KV, int MT>
+__global__ void __launch_bounds__(32 * kGroups * MT, MT == 1 ? 3 : 1)
+paged_attention_kernel(const __grid_constant__ AttnArgs a) {
+    using S = Shape<D, KV, MT>;
+    extern __shared__ __align__(128) uint8_t smem[];
+    uint8_t* ring = smem;
+    uint4* q_frag = reinterpret_cast<uint4*>(smem + S::kRing);                  // [MT][D / 16][32 lanes]
+    float* q_factor = reinterpret_cast<float*>(smem + S::kRing + S::kQueryBytes);  // what a row's products are multiplied with
+    long long* scratch = reinterpret_cast<long long*>(smem + S::kRing + S::kQueryBytes + S::kQueries * 4);
+    float4* key_consts = reinterpret_cast<float4*>(scratch + 40);                // [warp][16 keys]
+    int* bad = reinterpret_cast<int*>(key_consts + kGroups * MT * 16);           // [64 keys]
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int mt = warp % MT, group = warp / MT;
+    const int r0 = lane >> 2, c = lane & 3;
+    pdl_trigger();
+    pdl_wait();
+
+    long long total = 0, before = 0, tile = 0, tile_end = 0;
+    int unit = 0, ctas = 0;
+    find_unit<S::kQueries>(a, scratch, [&](long long sum) {
+        ctas = max(1, ctas_of(sum, a.grid));
+        return static_cast<int>(blockIdx.x) < ctas ? first_tile(sum, blockIdx.x, ctas) : sum;
+    }, total, unit, before);
+    if (unit < 0) return;  // (more CTAs than tiles)
+    tile = first_tile(total, blockIdx.x, ctas);
+    tile_end = first_tile(total, blockIdx.x + 1, ctas);
+
+    Segment g;
+    g.unit = unit;
+    g.limit = unit_limit<S::kQueries>(a, unit);
+    g.tiles = (g.limit + kTileKeys - 1) / kTileKeys;
+    {
+        const long long within = tile - before * a.cache.n_kv;
+        g.head = static_cast<int>(within / g.tiles);
+        g.tile0 = static_cast<int>(within - static_cast<long long>(g.head) * g.tiles);
+    }
+
+    while (true) {
+        g.tile1 = static_cast<int>(min(static_cast<long long>(g.tiles), g.tile0 + (tile_end - tile)));
+        const int b = g.unit / a.blocks, block = g.unit - b * a.blocks;
+        const int length = a.lengths[b];
+
+        // ---- a stage: 64 rows of K and of V, with their scales ----
+        const auto fetch = [&](int t, int stage) {
+            uint8_t* to = ring + stage * S::kStageBytes;
+            const uint32_t base = shared_u32(to);
+#pragma unroll
+            for (int i = threadIdx.x; i < 2 * kTileKeys * S::kChunks; i += S::kThreads) {
+                const int which = i / (kTileKeys * S::kChunks), rest = i - which * (kTileKeys * S::kChunks);
+                const int r = rest / S::kChunks, chunk = rest - r * S::kChunks, key = t * kTileKeys + r;
+                const long long at = key < g.limit ? a.cache.row(b, which, g.head, key) : -1;
+                copy16(base + which * (kTileKeys * S::kRowBytes) + S::place(r, chunk),
+                       static_cast<const uint8_t*>(a.pool) + (at < 0 ? 0 : at * S::kRowBytes + chunk * 16), at >= 0);
+            }
+            if constexpr (S::kEight) {
+                for (int i = threadIdx.x; i < 2 * kTileKeys; i += S::kThreads) {
+                    const int which = i / kTileKeys, r = i - which * kTileKeys, key = t * kTileKeys + r;
+                    const long long at = key < g.limit ? a.cache.row(b, which, g.head, key) : -1;
+                    copy4(base + 2 * kTileKeys * S::kRowBytes + i * 4, a.scales + (at < 0 ? 0 : at), at >= 0);
+                }
+            } else {
+                // (whether a row is there, where there are no scales to say so)
+                for (int i = threadIdx.x; i < kTileKeys; i += S::kThreads) {
+                    const int key = t * kTileKeys + i;
+                    const bool there = key < g.limit && a.cache.row(b, 0, g.head, key) >= 0;
+                    *reinterpret_cast<float*>(to + 2 * kTileKeys * S::kRowBytes + i * 4) = there ? 1.0f : 0.0f;
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        __syncthreads();  // the ring and the queries of the segment before are done with
+#pragma unroll
+        for (int s = 0; s < S::kStages - 1; ++s) {
+            if (g.tile0 + s < g.tile1) fetch(g.tile0 + s, s);
+            else asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+
+        // ---- the block's queries, in the order in which the products take them ----
+        // Lane c of a quad reads dims E (4 i + c) + 4 s .. + 3 of a key row (E elements to 16 bytes), so step E/4 i + s of the
+        // product takes the same dims of the query.  fp16 rows are brought to a largest magnitude in [1, 2) by a power of two.
+        constexpr int E = 16 / (S::kRowBytes / D), kPerChunk = E / 4;
+        for (int row = warp; row < S::kQueries; row += S::kThreads / 32) {
+            const int query = block * S::kQueries + row, i = query / a.group;
+            const bool there = i < a.rows;
+            float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (there && lane < D / 4) {
+                const int head = g.head * a.group + query - i * a.group;
+                const size_t at = (static_cast<size_t>(b) * a.rows + i) * a.q_stride + head * D + 4 * lane;
+                if (a.q_bf16) load4(static_cast<const __nv_bfloat16*>(a.q) + at, true, v);
+                else load4(static_cast<const __half*>(a.q) + at, true, v);
+            }
+            float back = 1.0f;
+            if constexpr (!S::kBf16) {
+                uint32_t largest = 0u;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) largest = max(largest, magnitude(v[j]));
+                largest = __reduce_max_sync(kFullMask, largest);
+                if (largest != 0u && largest < 0x7f800000u) {
+                    const int e = max(-120, min(120, static_cast<int>(largest >> 23) - 127));
+                    back = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+                    const float by = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] *= by;
+                }
+            }
+            if (lane < D / 4) {
+                const int dim = 4 * lane, chunk = dim / E, step = (chunk >> 2) * kPerChunk + (dim % E) / 4;
+                uint32_t* to = reinterpret_cast<uint32_t*>(q_frag + ((row >> 4) * (D / 16) + step) * 32 + (row & 7) * 4 + (chunk & 3)) + ((row >> 3) & 1);
+                to[0] = pack2<S::kBf16>(v[0], v[1]);
+                to[2] = pack2<S::kBf16>(v[2], v[3]);
+            }
+            if (lane == 0) q_factor[row] = back * a.scale * kLog2e;
+        }
+
+        // positions of this thread's two queries; one that does not exist sees nothing
+        int seen[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int i = (block * S::kQueries + mt * 16 + r0 + 8 * h) / a.group;
+            seen[h] = i < a.rows ? static_cast<int>(max(-1ll, static_cast<long long>(length) - a.rows + i)) : -1;
+        }
+        const int seen_by_all = static_cast<int>(max(-1ll, static_cast<long long>(length) - a.rows + min(a.rows - 1, block * S::kQueries / a.group)));
+
+        float o[D / 8][4], top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int n = 0; n < D / 8; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[n][j] = 0.0f;
+
+        int stage = 0;
+        for (int t = g.tile0; t < g.tile1; ++t) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 2) : "memory");
+            __syncthreads();
+            {
+                const int next = t + S::kStages - 1;
+                if (next < g.tile1) fetch(next, stage == 0 ? S::kStages - 1 : stage - 1);
+                else asm volatile("cp.async.commit_group;" ::: "memory");
+            }
+            const uint8_t* keys = ring + stage * S::kStageBytes;
+            const uint8_t* values = keys + kTileKeys * S::kRowBytes;
+            const float* consts = reinterpret_cast<const float*>(keys + 2 * kTileKeys * S::kRowBytes);
+            if (++stage == S::kStages) stage = 0;
+
+            // A weight of zero does not hide a V row that is no number from the product, so rows that some of the block's queries
+            // see and others do not are looked at first: one with such a value is taken out and told to those who see it.
+            const bool hidden = KV != SPEC_DTYPE_INT8 && (t + 1) * kTileKeys > seen_by_all + 1 && seen_by_all + 1 < g.limit;
+            if (hidden) {
+                uint8_t* rows_v = ring + (stage == 0 ? S::kStages - 1 : stage - 1) * S::kStageBytes + kTileKeys * S::kRowBytes;
+                for (int i = threadIdx.x; i < kTileKeys; i += S::kThreads) bad[i] = 0;
+                __syncthreads();
+                for (int i = threadIdx.x; i < kTileKeys * S::kChunks; i += S::kThreads)
+                    if (not_numbers<KV>(*reinterpret_cast<const uint4*>(rows_v + i * 16))) bad[i / S::kChunks] = 1;
+                __syncthreads();
+                for (int i = threadIdx.x; i < kTileKeys * S::kChunks; i += S::kThreads)
+                    if (bad[i / S::kChunks]) *reinterpret_cast<uint4*>(rows_v + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+                __syncthreads();
+            }
+
+            // what each of this warp's 16 keys brings: (factor of the product, exponent added, factor of the sum)
+            float4* mine = key_consts + warp * 16;
+            __syncwarp();
+            if (lane < 16) {
+                const int key = group * 16 + lane;
+                float4 k;
+                if constexpr (S::kEight) {
+                    const float sk = consts[key], sv = consts[kTileKeys + key];
+                    const bool there = sk != 0.0f;  // (no row's scale is zero; a row that is not there was filled with zeros)
+                    const bool number = magnitude(sv) < 0x7f800000u;  // (a row of V that is none makes the exponent none for who sees it, and no one else's sum)
+                    k = make_float4(sk, !there ? -INFINITY : number ? __log2f(sv) : NAN, there && number ? __fdividef(1.0f, sv) : 0.0f, 0.0f);
+                } else {
+                    k = make_float4(1.0f, consts[key] != 0.0f ? 0.0f : -INFINITY, 1.0f, 0.0f);
+                }
+                if (hidden && bad[key]) k.y = NAN;
+                mine[lane] = k;
+            }
+            __syncwarp();
+
+            float s[2][4];
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[n][j] = 0.0f;
+            const uint4* queries = q_frag + mt * (D / 16) * 32 + lane;
+#pragma unroll
+            for (int i = 0; i < S::kChunks / 4; ++i) {
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    const uint4 w = *reinterpret_cast<const uint4*>(keys + S::place(group * 16 + n * 8 + S::key_of(r0), 4 * i + c));
+                    if constexpr (S::kEight) {
+                        const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            uint32_t b0, b1;
+                            widen<KV, 1>(words[k], b0, b1);
+                            mma16816<S::kBf16>(s[n], queries[(4 * i + k) * 32], b0, b1);
+                        }
+                    } else {
+                        mma16816<S::kBf16>(s[n], queries[(2 * i) * 32], w.x, w.y);
+                        mma16816<S::kBf16>(s[n], queries[(2 * i + 1) * 32], w.z, w.w);
+                    }
+                }
+            }
+            // ---- exponents, their running maximum, weights ----
+            const float factor[2] = {q_factor[mt * 16 + r0], q_factor[mt * 16 + r0 + 8]};
+            const bool masked = t * kTileKeys + group * 16 + 15 > seen_by_all;
+            float inv[2][2];
+            float now[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int key = n * 8 + S::key_of(2 * c + x);
+                    const float4 k = mine[key];
+                    inv[n][x] = k.z;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float e = fmaf(s[n][2 * h + x], k.x * factor[h], k.y);
+                        if (k.y == -INFINITY || (masked && t * kTileKeys + group * 16 + key > seen[h])) e = -INFINITY;
+                        s[n][2 * h + x] = e;
+                        now[h] = fmaxf(now[h], e);
+                    }
+                }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                now[h] = fmaxf(now[h], __shfl_xor_sync(kFullMask, now[h], 1));
+                now[h] = fmaxf(now[h], __shfl_xor_sync(kFullMask, now[h], 2));
+            }
+            if (__any_sync(kFullMask, now[0] > top[0] + kSlack || now[1] > top[1] + kSlack)) {
+                float shrink[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float higher = fmaxf(top[h], now[h]);
+                    shrink[h] = top[h] == -INFINITY ? 0.0f : exp2f(top[h] - higher);
+                    top[h] = higher;
+                    sum[h] *= shrink[h];
+                }
+#pragma unroll
+                for (int n = 0; n < D / 8; ++n) {
+                    o[n][0] *= shrink[0];
+                    o[n][1] *= shrink[0];
+                    o[n][2] *= shrink[1];
+                    o[n][3] *= shrink[1];
+                }
+            }
+            uint4 p;
+            {
+                const float from[2] = {top[0] == -INFINITY ? 0.0f : top[0], top[1] == -INFINITY ? 0.0f : top[1]};
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        s[n][j] = exp2f(s[n][j] - from[j >> 1]);
+                        sum[j >> 1] = fmaf(s[n][j], inv[n][j & 1], sum[j >> 1]);
+                    }
+                p.x = pack2<S::kBf16>(s[0][0], s[0][1]);
+                p.y = pack2<S::kBf16>(s[0][2], s[0][3]);
+                p.z = pack2<S::kBf16>(s[1][0], s[1][1]);
+                p.w = pack2<S::kBf16>(s[1][2], s[1][3]);
+            }
+            // ---- weights times values: key 2 c, 2 c + 1 (and + 8) of the product are the columns of the scores ----
+            const uint32_t v_base = shared_u32(values);
+            const int v_row = group * 16 + ((lane >> 3) & 1) * 8 + S::key_of(lane & 7);
+#pragma unroll
+            for (int i = 0; i < S::kChunks / 2; ++i) {
+                uint32_t w[4];
+                ldmatrix4_trans(w, v_base + S::place(v_row, 2 * i + (lane >> 4)));
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if constexpr (S::kEight) {
+                        uint32_t even0, odd0, even1, odd1;
+                        widen<KV, 2>(w[2 * h], even0, odd0);
+                        widen<KV, 2>(w[2 * h + 1], even1, odd1);
+                        mma16816<S::kBf16>(o[2 * (2 * i + h)], p, even0, even1);
+                        mma16816<S::kBf16>(o[2 * (2 * i + h) + 1], p, odd0, odd1);
+                    } else {
+                        mma16816<S::kBf16>(o[2 * i + h], p, w[2 * h], w[2 * h + 1]);
+                    }
+                }
+            }
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            sum[h] += __shfl_xor_sync(kFullMask, sum[h], 1);
+            sum[h] += __shfl_xor_sync(kFullMask, sum[h], 2);
+        }
+        // ---- the four groups' states become one: groups 2, 3 into 0, 1, then 1 into 0 ----
+        float* merge = reinterpret_cast<float*>(ring);
+#pragma unroll
+        for (int step = kGroups / 2; step > 0; step >>= 1) {
+            __syncthreads();
+            if (group >= step && group < 2 * step) {
+                float* to = merge + ((group - step) * MT + mt) * 16 * (D + 2) + lane;
+#pragma unroll
+                for (int n = 0; n < D / 8; ++n)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) to[(n * 4 + j) * 32] = o[n][j];
+                if (c == 0) {
+                    float* ml = merge + ((group - step) * MT + mt) * 16 * (D + 2) + 16 * D;
+                    ml[r0] = top[0];
+                    ml[r0 + 8] = top[1];
+                    ml[16 + r0] = sum[0];
+                    ml[16 + r0 + 8] = sum[1];
+                }
+            }
+            __syncthreads();
+            if (group < step) {
+                const float* from = merge + (group * MT + mt) * 16 * (D + 2);
+                float keep[2], take[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float other = from[16 * D + r0 + 8 * h], higher = fmaxf(top[h], other);
+                    keep[h] = top[h] == -INFINITY ? 0.0f : exp2f(top[h] - higher);
+                    take[h] = other == -INFINITY ? 0.0f : exp2f(other - higher);
+                    sum[h] = sum[h] * keep[h] + from[16 * D + 16 + r0 + 8 * h] * take[h];
+                    top[h] = higher;
+                }
+#pragma unroll
+                for (int n = 0; n < D / 8; ++n)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[n][j] = o[n][j] * keep[j >> 1] + from[lane + (n * 4 + j) * 32] * take[j >> 1];
+            }
+        }
+        if (group == 0) {
+            const bool whole = g.tile0 == 0 && g.tile1 == g.tiles;
+            const long long slot = static_cast<long long>(blockIdx.x) + static_cast<long long>(g.unit) * a.cache.n_kv + g.head;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int row = mt * 16 + r0 + 8 * h, query = block * S::kQueries + row, i = query / a.group;
+                if (i >= a.rows) continue;
+                const float by = whole ? (sum[h] == 0.0f ? 0.0f : __fdividef(1.0f, sum[h])) : 1.0f;
+                const size_t at = ((static_cast<size_t>(b) * a.rows + i) * a.n_heads + g.head * a.group + query - i * a.group) * D;
+                float* part = a.partial + (slot * S::kQueries + row) * D;
+                if (!whole && c == 0) a.partial_ml[slot * S::kQueries + row] = make_float2(top[h], sum[h]);
+#pragma unroll
+                for (int n = 0; n < D / 8; n += 2) {
+                    // 8-bit rows: tiles n, n + 1 hold the even and the odd dims of 16; 16-bit rows: 8 dims each
+                    if constexpr (S::kEight) {
+                        const float v[4] = {o[n][2 * h] * by, o[n + 1][2 * h] * by, o[n][2 * h + 1] * by, o[n + 1][2 * h + 1] * by};
+                        const int dim = 8 * n + 4 * c;
+                        if (!whole) *reinterpret_cast<float4*>(part + dim) = *reinterpret_cast<const float4*>(v);
+                        else if (a.q_bf16) store4(static_cast<__nv_bfloat16*>(a.out) + at + dim, true, v);
+                        else store4(static_cast<__half*>(a.out) + at + dim, true, v);
+                    } else {
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) {
+                            const int dim = 8 * (n + m) + 2 * c;
+                            const float x = o[n + m][2 * h] * by, y = o[n + m][2 * h + 1] * by;
+                            if (!whole) *reinterpret_cast<float2*>(part + dim) = make_float2(x, y);
+                            else if (a.q_bf16) *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(a.out) + at + dim) = pack2<true>(x, y);
+                            else *reinterpret_cast<uint32_t*>(static_cast<__half*>(a.out) + at + dim) = pack2<false>(x, y);
+                        }
+                    }
+                }
+            }
+        }
+        // ---- the next segment of the run ----
+        tile += g.tile1 - g.tile0;
+        if (tile >= tile_end) return;
+        g.tile0 = 0;
+        if (++g.head == a.cache.n_kv) {
+            g.head = 0;
+            do {
+                ++g.unit;
+                g.limit = unit_limit<S::kQueries>(a, g.unit);
+            } while (g.limit == 0);
+            g.tiles = (g.limit + kTileKeys - 1) / kTileKeys;
+        }
+    }
+}
+
+// Joins the states of a segment that several CTAs had, in their order; a segment without a key gets its zeros here.  A warp per
+// query, grid = (segments, queries of a block / 4).
+template <int D, int QT>
+__global__ void __launch_bounds__(128)
+join_kernel(const __grid_constant__ AttnArgs a) {
+    __shared__ long long scratch[40];
+    pdl_trigger();
+    pdl_wait();
+    const int unit = blockIdx.x / a.cache.n_kv, head = blockIdx.x - unit * a.cache.n_kv;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int b = unit / a.blocks, block = unit - b * a.blocks;
+    const int row = blockIdx.y * 4 + warp, query = block * QT + row, i = query / a.group;
+    const int limit = unit_limit<QT>(a, unit), tiles = (limit + kTileKeys - 1) / kTileKeys;
+    long long total = 0, front = 0;
+    {  // tiles of all units, and of those before this one
+        long long all = 0, mine = 0;
+        for (int u = threadIdx.x; u < a.units; u += 128) {
+            const int n = (unit_limit<QT>(a, u) + kTileKeys - 1) / kTileKeys;
+            all += n;
+            if (u < unit) mine += n;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            all += __shfl_xor_sync(kFullMask, all, o);
+            mine += __shfl_xor_sync(kFullMask, mine, o);
+        }
+        if (lane == 0) {
+            scratch[warp] = all;
+            scratch[4 + warp] = mine;
+        }
+        __syncthreads();
+        for (int w = 0; w < 4; ++w) {
+            total += scratch[w];
+            front += scratch[4 + w];
+        }
+        total *= a.cache.n_kv;
+        front = front * a.cache.n_kv + static_cast<long long>(head) * tiles;
+    }
+    if (i >= a.rows) return;
+    const size_t at = ((static_cast<size_t>(b) * a.rows + i) * a.n_heads + head * a.group + query - i * a.group) * D;
+    constexpr int kPer = D / 32;
+    float v[kPer] = {};
+    if (tiles > 0) {
+        const int ctas = ctas_of(total, a.grid), first = owner_of(total, front, ctas), last = owner_of(total, front + tiles - 1, ctas);
+        if (first == last) return;  // (written by the CTA that had all of it)
+        const long long slot0 = static_cast<long long>(unit) * a.cache.n_kv + head;
+        float top = -INFINITY;
+        for (int p = first + lane; p <= last; p += 32) top = fmaxf(top, a.partial_ml[(slot0 + p) * QT + row].x);
+        top = warp_max(top);
+        float sum = 0.0f;
+#pragma unroll 4
+        for (int p = first; p <= last; ++p) {
+            const float2 ml = a.partial_ml[(slot0 + p) * QT + row];
+            const float w = ml.x == -INFINITY ? 0.0f : exp2f(ml.x - top);
+            sum = fmaf(w, ml.y, sum);
+            const float* part = a.partial + ((slot0 + p) * QT + row) * D + kPer * lane;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) v[j] = fmaf(w, part[j], v[j]);
+        }
+        const float by = sum == 0.0f ? 0.0f : __fdividef(1.0f, sum);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) v[j] *= by;
+    }
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        if (a.q_bf16) static_cast<__nv_bfloat16*>(a.out)[at + kPer * lane + j] = __float2bfloat16_rn(v[j]);
+        else static_cast<__half*>(a.out)[at + kPer * lane + j] = __float2half_rn(v[j]);
+    }
+}
+
+// 16-query tiles of a block: as many as the queries of a (sequence, KV head) fill, at most four.
+int query_tiles(int rows, int group) {
+    const long long queries = static_cast<long long>(rows) * group;
+    return queries <= 16 ? 1 : queries <= 32 ? 2 : 4;
+}
+
+size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
+
+template <int D, int KV, int MT>
+int launch(const AttnArgs& args, cudaStream_t stream) {
+    using S = Shape<D, KV, MT>;
+    static std::atomic<unsigned long long> configured{0};
+    int status = allow_shared_memory(configured, paged_attention_kernel<D, KV, MT>, S::kSmem);
+    if (status != SPEC_OK) return status;
+    AttnArgs a = args;
+    constexpr int per_sm = MT == 1 ? 3 : 1;
+    a.grid = 148 * per_sm;
+    status = launch_pdl(paged_attention_kernel<D, KV, MT>, dim3(a.grid), dim3(S::kThreads), S::kSmem, stream, a);
+    if (status != SPEC_OK) return status;
+    return launch_pdl(join_kernel<D, S::kQueries>, dim3(a.units * a.cache.n_kv, S::kQueries / 4), dim3(128), 0, stream, a);
+}
+
+template <int D, int KV>
+int launch_tiles(const AttnArgs& a, cudaStream_t stream) {
+    const int mt = query_tiles(a.rows, a.group);
+    return mt == 1 ? launch<D, KV, 1>(a, stream) : mt == 2 ? launch<D, KV, 2>(a, stream) : launch<D, KV, 4>(a, stream);
+}
+
+template <int D>
+int launch_kv(const AttnArgs& a, int kv_dtype, cudaStream_t stream) {
+    switch (kv_dtype) {
+        case SPEC_DTYPE_FP16: return launch_tiles<D, SPEC_DTYPE_FP16>(a, stream);
+        case SPEC_DTYPE_BF16: return launch_tiles<D, SPEC_DTYPE_BF16>(a, stream);
+        case SPEC_DTYPE_E4M3: return launch_tiles<D, SPEC_DTYPE_E4M3>(a, stream);
+        default: return launch_tiles<D, SPEC_DTYPE_INT8>(a, stream);
+    }
+}
+
+bool fits(int batch, int rows, int n_heads, int n_kv_heads, int d_head) {
+    return batch >= 1 && batch <= 65535 && rows >= 1 && rows <= 65536 && n_kv_heads >= 1 && n_kv_heads <= 1024 && n_heads >= n_kv_heads &&
+           n_heads % n_kv_heads == 0 && n_heads <= 65536 && (d_head == 64 || d_head == 128);
+}
+long long units_of(int batch, int rows, int group, int queries) { return static_cast<long long>(batch) * ((static_cast<long long>(rows) * group + queries - 1) / queries); }
+
+}  // namespace
+}  // namespace spec
+
+extern "C" size_t spec_paged_attention_workspace_bytes(int batch, int rows, int n_heads, int n_kv_heads, int d_head) {
+    using namespace spec;
+    if (!fits(batch, rows, n_heads, n_kv_heads, d_head)) return 0;
+    const int group = n_heads / n_kv_heads, queries = 16 * query_tiles(rows, group);
+    const size_t slots = kMostCtas + static_cast<size_t>(units_of(batch, rows, group, queries)) * n_kv_heads;
+    return align256(slots * queries * d_head * 4) + align256(slots * queries * 8);
+}
+
+extern "C" int spec_paged_attention(const void* q, int dtype, int64_t q_stride, const void* pool, const float* scales, int kv_dtype, int pages,
+                                    int page_size, const int32_t* page_table, int max_pages, const int32_t* lengths, int batch, int rows, int n_heads,
+                                    int n_kv_heads, int d_head, float scale, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace spec;
+    const char* who = "spec_paged_attention";
+    if (dtype != SPEC_DTYPE_BF16 && dtype != SPEC_DTYPE_FP16) return fail(SPEC_ERR_BAD_ARG, "%s: dtype %d (bf16 or fp16)", who, dtype);
+    if (rows < 0 || batch < 0) return fail(SPEC_ERR_BAD_ARG, "%s: batch=%d rows=%d", who, batch, rows);
+    if (rows == 0 || batch == 0) return SPEC_OK;
+    if (!fits(batch, rows, n_heads, n_kv_heads, d_head)) return fail(SPEC_ERR_BAD_ARG, "%s: batch=%d rows=%d n_heads=%d n_kv_heads=%d d_head=%d", who, batch, rows, n_heads, n_kv_heads, d_head);
+    AttnArgs a{};
+    const int status = check_paged(who, pool, scales, kv_dtype, pages, page_size, n_kv_heads, d_head, page_table, max_pages, batch, &a.cache);
+    if (status != SPEC_OK) return status;
+    if ((kv_dtype == SPEC_DTYPE_FP16 || kv_dtype == SPEC_DTYPE_BF16) && kv_dtype != dtype) return fail(SPEC_ERR_BAD_ARG, "%s: a 16-bit cache needs queries of its own type", who);
+    if (!(scale > -3.0e38f && scale < 3.0e38f)) return fail(SPEC_ERR_BAD_ARG, "%s: scale must be finite", who);
+    if (!q || !out || !lengths) return fail(SPEC_ERR_BAD_ARG, "%s: null pointer", who);
+    if (!aligned_to(q, 8) || !aligned_to(out, 8) || q_stride % 4 || !aligned_to(lengths, 4)) return fail(SPEC_ERR_BAD_ARG, "%s: q and out have to start on 8 bytes, q's rows too", who);
+    if (q_stride < static_cast<int64_t>(n_heads) * d_head) return fail(SPEC_ERR_BAD_ARG, "%s: q's row stride is below the heads' elements", who);
+    a.group = n_heads / n_kv_heads;
+    const int queries = 16 * query_tiles(rows, a.group);
+    const long long units = units_of(batch, rows, a.group, queries);
+    if (units * n_kv_heads > 0x7fffffff - kMostCtas) return fail(SPEC_ERR_BAD_ARG, "%s: too many rows for one call", who);
+    if (!workspace || workspace_bytes < spec_paged_attention_workspace_bytes(batch, rows, n_heads, n_kv_heads, d_head) || !aligned_to(workspace, 256))
+        return fail(SPEC_ERR_BAD_ARG, "%s: workspace missing, too small or not 256-byte aligned", who);
+    const size_t slots = kMostCtas + static_cast<size_t>(units) * n_kv_heads;
+    a.pool = pool;
+    a.scales = scales;
+    a.q = q;
+    a.out = out;
+    a.lengths = lengths;
+    a.partial = static_cast<float*>(workspace);
+    a.partial_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + align256(slots * queries * d_head * 4));
+    a.q_stride = q_stride;
+    a.scale = scale;
+    a.batch = batch;
+    a.rows = rows;
+    a.n_heads = n_heads;
+    a.units = static_cast<int>(units);
+    a.blocks = a.units / batch;
+    a.q_bf16 = dtype == SPEC_DTYPE_BF16;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return d_head == 64 ? launch_kv<64>(a, kv_dtype, st) : launch_kv<128>(a, kv_dtype, st);
+}
