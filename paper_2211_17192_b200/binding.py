@@ -59,6 +59,9 @@ def lib():
                     loader.exec_module(calls)
                     address = lambda f: ctypes.cast(f, ctypes.c_void_p).value
                     calls.bind(address(handle.spec_verify_sample_truncated), address(handle.spec_sample), torch.float32, torch.int32, torch.uint8)
+                    calls.bind_operators(
+                        tuple(address(getattr(handle, "spec_" + f)) for f in ("quantize_fp8", "norm_fp8", "linear_fp8", "kv_append", "kv_read", "paged_attention")),
+                        (torch.float32, torch.bfloat16, torch.float16, torch.float8_e4m3fn, torch.int8, torch.int32, torch.uint8))
                     _calls = calls
                 _lib = handle
     return _lib
@@ -363,6 +366,18 @@ def _operand(t, name, dtypes, shape=None, contiguous=True):
     return t.data_ptr()
 
 
+def _plain(call, first, *args):
+    """Whether the module of csrc/calls.c has made the call (with all of its tensors given, and `first` among them on a GPU); one
+    that it leaves is made below, where what is wrong with it is said."""
+    lib()
+    if _calls is None or not getattr(first, "is_cuda", False):
+        return False
+    status = getattr(_calls, call)(*args, torch._C._cuda_getDevice(), _stream())
+    if status:
+        _check(status)
+    return status == 0
+
+
 def _optional(t, name, dtypes, shape=None):
     return None if t is None else _operand(t, name, dtypes, shape)
 
@@ -395,6 +410,8 @@ def _pool_args(pool, scales, page_table, batch):
 def spec_quantize_fp8(x, codes=None, scales=None):
     """Rows in e4m3 with a scale each: x [rows, d] fp32, bf16 or fp16 CUDA -> (codes [rows, d] float8_e4m3fn, scales [rows] fp32),
     value = code * scale.  Also how the weights of `spec_linear_fp8` are made."""
+    if codes is not None and scales is not None and _plain("quantize", x, x, codes, scales):
+        return codes, scales
     _need(isinstance(x, torch.Tensor) and x.dim() == 2, "x must be [rows, d]")
     where = _operand(x, "x", _FLOATS)
     rows, d = x.shape
@@ -410,6 +427,8 @@ def spec_norm_fp8(x, gain, eps=1e-6, residual=None, h=None, codes=None, scales=N
     rmsnorm(h) * gain; x [rows, d] fp32, bf16 or fp16, gain [d] fp32, residual and h [rows, d] fp32 or of x's type.
     Returns (codes, scales, h); h is allocated when a residual is given without it, may be the residual itself, and is
     None when neither is given."""
+    if codes is not None and scales is not None and _plain("norm", x, x, gain, eps, residual, h, codes, scales):
+        return codes, scales, h
     _need(isinstance(x, torch.Tensor) and x.dim() == 2, "x must be [rows, d]")
     where = _operand(x, "x", _FLOATS)
     rows, d = x.shape
@@ -434,6 +453,8 @@ def spec_linear_fp8(x, x_scales, w, w_scales, bias=None, act="none", residual=No
     rows first); bias [n_w] fp32; residual and y [rows, n_out] of one type, y is allocated in the residual's type or `dtype`
     when not given and may be the residual."""
     _need(act in ACTIVATIONS, f"act must be one of {', '.join(ACTIVATIONS)}")
+    if y is not None and _plain("linear", x, x, x_scales, w, w_scales, bias, ACTIVATIONS[act], residual, y):
+        return y
     _need(isinstance(x, torch.Tensor) and x.dim() == 2 and isinstance(w, torch.Tensor) and w.dim() == 2 and x.shape[1] == w.shape[1],
           "x must be [rows, k] and w [n_w, k]")
     (rows, k), n_w = x.shape, w.shape[0]
@@ -457,6 +478,8 @@ def spec_kv_append(k, v, pool, scales, page_table, start, counts=None, rope=None
     bf16 or fp16, parts of one projection's output or tensors of their own; pool [pages, 2, kv heads, page size, d_head];
     scales [pages, 2, kv heads, page size] fp32 for 8-bit pools, else None; page_table [B, max_pages], start [B],
     counts [B] int32.  Row i of sequence b goes to position start[b] + i if i < counts[b].  Returns q_out (None without q)."""
+    if (q is None or q_out is not None) and _plain("append", k, k, v, pool, scales, page_table, start, counts, rope, q, q_out):
+        return q_out
     _need(isinstance(k, torch.Tensor) and k.dim() == 4, "k must be [B, rows, heads, d_head]")
     batch, rows, n_kv, d = k.shape
     where, at, kv_dtype, pages, page_size, table, width, pool_heads, pool_d = _pool_args(pool, scales, page_table, batch)
@@ -485,6 +508,8 @@ def spec_kv_read(pool, scales, page_table, start, rows, counts=None, dtype=torch
     """The cached rows at start[b] .. start[b] + counts[b] - 1 (`rows` of them without counts) of every sequence, widened:
     (k, v) [B, rows, kv heads, d_head] of `dtype`, zeros where there is no row, or into the tensors given, whose other rows
     stay as they are."""
+    if k is not None and v is not None and _plain("read", pool, pool, scales, page_table, start, rows, counts, k, v):
+        return k, v
     _need(isinstance(page_table, torch.Tensor) and page_table.dim() == 2, "page_table must be [B, max_pages]")
     batch = page_table.shape[0]
     where, at, kv_dtype, pages, page_size, table, width, n_kv, d = _pool_args(pool, scales, page_table, batch)
@@ -506,6 +531,9 @@ def spec_paged_attention(q, pool, scales, page_table, lengths, scale=None, out=N
     bf16 or fp16, the cache as in `spec_kv_append`, lengths [B] int32 the tokens cached with the new ones; row i sees the keys at
     and before position lengths[b] - rows + i.  scale defaults to d_head ** -0.5.  Returns out, of q's shape and type; it and
     the workspace are allocated when not given."""
+    if out is not None and workspace is not None and \
+            _plain("attention", q, q, pool, scales, page_table, lengths, q.shape[-1] ** -0.5 if scale is None else scale, out, workspace):
+        return out
     _need(isinstance(q, torch.Tensor) and q.dim() == 4, "q must be [B, rows, heads, d_head]")
     batch, rows, heads, d = q.shape
     where, at, kv_dtype, pages, page_size, table, width, n_kv, pool_d = _pool_args(pool, scales, page_table, batch)
