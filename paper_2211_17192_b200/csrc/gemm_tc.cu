@@ -363,6 +363,17 @@ struct MapKey {
 
 }  // namespace
 
+int encode_map(CUtensorMapDataType type, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box,
+               CUtensorMapSwizzle swizzle, CUtensorMap* out) {
+    EncodeFn fn = encode_fn();
+    if (!fn) return fail(SPEC_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
+    const cuuint32_t elem[5] = {1, 1, 1, 1, 1};
+    const CUresult res = fn(out, type, static_cast<cuuint32_t>(rank), const_cast<void*>(base), dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (res != CUDA_SUCCESS) return fail(SPEC_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", static_cast<int>(res));
+    return SPEC_OK;
+}
+
 // Tensor maps are pure functions of (address, shape, box): cached process-wide.
 int cached_bf16_map(const void* base, int rows, int cols, int box_rows, bool swizzle, CUtensorMap* out) {
     static std::mutex mu;
@@ -657,6 +668,7 @@ extern "C" int spec_timeout_drill(void* stream) {
 
 extern "C" int spec_device_error(void) {
     const int gemm = spec::gemm_tc_take_error(), wide = spec::gemm_wide_take_error(), pass = spec::pass_take_error(), attn = spec::attention_take_error(),
-              small = spec::small_pass_take_error(), tiny = spec::cluster_pass_take_error(), linear = spec::linear_fp8_take_error();
-    return gemm ? gemm : wide ? wide : pass ? pass : attn ? attn : small ? small : tiny ? tiny : linear;
+              small = spec::small_pass_take_error(), tiny = spec::cluster_pass_take_error(), linear = spec::linear_fp8_take_error(),
+              paged = spec::paged_attention_take_error();
+    return gemm ? gemm : wide ? wide : pass ? pass : attn ? attn : small ? small : tiny ? tiny : linear ? linear : paged;
 }

@@ -283,23 +283,10 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
 
 // A matrix of codes [planes][rows][k] in boxes of [box_planes][box_rows][128], 128-byte swizzle on the way in, zeros past its edges.
 int codes_map(const void* base, int planes, int rows, int k, int box_planes, int box_rows, CUtensorMap* out) {
-    using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-    static const EncodeFn encode = [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) p = nullptr;
-        return reinterpret_cast<EncodeFn>(p);
-    }();
-    if (!encode) return fail(SPEC_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
     const cuuint64_t dims[3] = {static_cast<cuuint64_t>(k), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(planes)};
     const cuuint64_t strides[2] = {static_cast<cuuint64_t>(k), static_cast<cuuint64_t>(k) * rows};
     const cuuint32_t box[3] = {kBlockK, static_cast<cuuint32_t>(box_rows), static_cast<cuuint32_t>(box_planes)};
-    const cuuint32_t elem[3] = {1, 1, 1};
-    const CUresult res = encode(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, box_planes ? 3 : 2, const_cast<void*>(base), dims, strides, box, elem,
-                                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (res != CUDA_SUCCESS) return fail(SPEC_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", static_cast<int>(res));
-    return SPEC_OK;
+    return encode_map(CU_TENSOR_MAP_DATA_TYPE_UINT8, box_planes ? 3 : 2, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, out);
 }
 
 int launch_small(const void* x, const void* w, int k, LinearArgs a, cudaStream_t stream) {

@@ -13,20 +13,26 @@
 // the page table); a segment that several CTAs share leaves (maximum, sum, weighted rows) per CTA in the workspace, and a second
 // kernel joins them in order.  No atomics: the same bits every time.
 //
-// A CTA has four groups of warps; a group takes 16 of a tile's 64 keys, a warp of it 16 queries.  Tiles come through a ring of
-// cp.async stages; rows that are not there (past the limit, or on a page outside the pool) are filled with zeros and masked.
+// A CTA has four groups of warps; a group takes 16 of a tile's 64 keys, a warp of it 16 queries.  One more warp asks for the tiles
+// of the whole run, segment after segment, by TMA (halves of 32 keys, which never straddle a page, with the shared-memory
+// swizzle), through a ring of stages with a barrier to fill and one to free each; the others never wait for one another within a segment.
 #include <algorithm>
 
 #include "paged.cuh"
+#include "tc_util.cuh"
 
 namespace spec {
 namespace {
+
+using namespace tc;
 
 constexpr int kTileKeys = 64;
 constexpr int kGroups = 4;       // warps along a tile's keys, 16 keys each
 constexpr int kMostCtas = 592;   // 148 SMs x 4
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.0f;   // the running maximum may lag by this: w <= 2^8 stays in fp16's range
+
+__device__ int g_paged_error;  // set when the bounded wait for a tile or for its place ran out (0 = none)
 
 struct AttnArgs {
     Paged cache;
@@ -43,13 +49,20 @@ struct AttnArgs {
     int q_bf16, grid;
 };
 
-__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool there) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
+// Copies that count their bytes on a barrier: a box of 32 rows of a plane (K or V of a page and head), and a run of bytes.
+__device__ __forceinline__ void load_box(void* to, const CUtensorMap* map, int x, int row, int plane, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(smem_u32(to)), "l"(map), "r"(x), "r"(row), "r"(plane), "r"(smem_u32(bar))
+        : "memory");
 }
-__device__ __forceinline__ void copy4(uint32_t to, const void* from, bool there) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(there ? 4 : 0) : "memory");
+__device__ __forceinline__ void load_bulk(void* to, const void* from, int bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(smem_u32(to)), "l"(from), "r"(bytes), "r"(smem_u32(bar)) : "memory");
 }
-__device__ __forceinline__ uint32_t shared_u32(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
 
 template <bool BF16>
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint4& a, uint32_t b0, uint32_t b1) {
@@ -183,105 +196,175 @@ struct Shape {
     static constexpr bool kEight = KV == SPEC_DTYPE_E4M3 || KV == SPEC_DTYPE_INT8;
     static constexpr bool kBf16 = KV == SPEC_DTYPE_BF16;
     static constexpr int kRowBytes = D * (kEight ? 1 : 2);
+    static constexpr int kBoxBytes = kRowBytes < 128 ? kRowBytes : 128;  // of a row in one copy: what the swizzle spans
+    static constexpr int kBoxes = kRowBytes / kBoxBytes;
     static constexpr int kChunks = kRowBytes / 16;
     static constexpr int kQueries = 16 * MT;
-    static constexpr int kThreads = 32 * kGroups * MT;
-    static constexpr int kStageBytes = 2 * kTileKeys * kRowBytes + 2 * kTileKeys * 4;
-    static constexpr int kStages = 3;
+    static constexpr int kComputeWarps = kGroups * MT;
+    static constexpr int kThreads = 32 * (kComputeWarps + 1);  // and the warp that asks for the tiles
+    static constexpr int kOperandBytes = kTileKeys * kRowBytes;  // K or V of a tile
+    static constexpr int kStageBytes = 2 * kOperandBytes;
+    static constexpr int kScaleBytes = kEight ? 2 * kTileKeys * 4 : 0;
     static constexpr int kQueryBytes = kQueries * D * 2;
     static constexpr int kMerge = 2 * MT * 16 * (D + 2) * 4;  // two groups' states
-    static constexpr int kRing = kStages * kStageBytes > kMerge ? kStages * kStageBytes : kMerge;
-    static constexpr int kSmem = kRing + kQueryBytes + kQueries * 4 + 40 * 8 + kGroups * MT * 16 * 16 + kTileKeys * 4;
-    // Place of 16-byte chunk c of row r: rows whose chunks meet in the reads below lie in different banks.
-    static __device__ __forceinline__ int place(int r, int c) { return r * kRowBytes + ((kRowBytes == 64 ? c ^ ((r >> 1) & 3) : c ^ (r & 7)) << 4); }
+    static constexpr int kPerSm = MT == 1 ? (kRowBytes <= 128 ? 3 : 2) : 1;
+    static constexpr int kFixed = kMerge + kQueryBytes + kQueries * 4 + 40 * 8 + kComputeWarps * 16 * 16 + 1024 /* alignment */ + 256 /* barriers, notes */;
+    static constexpr int kStagesThatFit = ((227 * 1024 + 1024) / kPerSm - 1024 - kFixed) / (kStageBytes + kScaleBytes);
+    static constexpr int kStages = kStagesThatFit < 8 ? kStagesThatFit : 8;
+    static constexpr int kSmem = kStages * (kStageBytes + kScaleBytes) + kFixed;
+    static_assert(kStages >= 2, "a ring");
+    // Place of 16-byte chunk c of row r in a K or V tile, as the copies' swizzle leaves it: rows whose chunks meet in the reads
+    // below lie in different banks.
+    static __device__ __forceinline__ int place(int r, int c) {
+        if constexpr (kBoxBytes == 64) return r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
+        else return (c >> 3) * (kTileKeys * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+    }
     // Which of eight keys a lane quad n reads, and column n of a score tile stands for: neighbours differ in the bit that moves a
     // row's chunks to the other half of the banks.
-    static __device__ __forceinline__ int key_of(int n) { return kRowBytes == 64 ? n : (n & 1) * 4 + (n >> 1); }
+    static __device__ __forceinline__ int key_of(int n) { return kBoxBytes == 64 ? n : (n & 1) * 4 + (n >> 1); }
 };
 
-template <int D, int KV, int MT>
-__global__ void __launch_bounds__(32 * kGroups * MT, MT == 1 ? 3 : 1)
-paged_attention_kernel(const __grid_constant__ AttnArgs a) {
-    using S = Shape<D, KV, MT>;
-    extern __shared__ __align__(128) uint8_t smem[];
-    uint8_t* ring = smem;
-    uint4* q_frag = reinterpret_cast<uint4*>(smem + S::kRing);                  // [MT][D / 16][32 lanes]
-    float* q_factor = reinterpret_cast<float*>(smem + S::kRing + S::kQueryBytes);  // what a row's products are multiplied with
-    long long* scratch = reinterpret_cast<long long*>(smem + S::kRing + S::kQueryBytes + S::kQueries * 4);
-    float4* key_consts = reinterpret_cast<float4*>(scratch + 40);                // [warp][16 keys]
-    int* bad = reinterpret_cast<int*>(key_consts + kGroups * MT * 16);           // [64 keys]
+// The tiles of a CTA's run, segment by segment.
+template <int QT>
+struct Run {
+    long long left;  // tiles, the present segment's among them
+    Segment g;
+    __device__ __forceinline__ void open(const AttnArgs& a) {  // what follows from unit
+        g.limit = unit_limit<QT>(a, g.unit);
+        g.tiles = (g.limit + kTileKeys - 1) / kTileKeys;
+    }
+    __device__ __forceinline__ void close() { g.tile1 = static_cast<int>(min(static_cast<long long>(g.tiles), g.tile0 + left)); }
+    __device__ __forceinline__ bool next(const AttnArgs& a) {
+        left -= g.tile1 - g.tile0;
+        if (left <= 0) return false;
+        g.tile0 = 0;
+        if (++g.head == a.cache.n_kv) {
+            g.head = 0;
+            do {
+                ++g.unit;
+                open(a);
+            } while (g.limit == 0);
+        }
+        close();
+        return true;
+    }
+};
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int mt = warp % MT, group = warp / MT;
-    const int r0 = lane >> 2, c = lane & 3;
+template <int THREADS>
+__device__ __forceinline__ void compute_sync() { asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory"); }
+
+template <int D, int KV, int MT>
+__global__ void __launch_bounds__(Shape<D, KV, MT>::kThreads, Shape<D, KV, MT>::kPerSm)
+paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ AttnArgs a) {
+    using S = Shape<D, KV, MT>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    float* ring_scales = reinterpret_cast<float*>(ring + S::kStages * S::kStageBytes);  // [stage][K, V][64]
+    float* merge = reinterpret_cast<float*>(ring + S::kStages * (S::kStageBytes + S::kScaleBytes));
+    uint4* q_frag = reinterpret_cast<uint4*>(merge + S::kMerge / 4);                 // [MT][D / 16][32 lanes]
+    float4* key_consts = reinterpret_cast<float4*>(q_frag + S::kQueryBytes / 16);                               // [warp][16 keys]
+    float* q_factor = reinterpret_cast<float*>(key_consts + S::kComputeWarps * 16);  // what a row's products are multiplied with
+    long long* scratch = reinterpret_cast<long long*>(q_factor + S::kQueries);
+    uint64_t* full_bar = reinterpret_cast<uint64_t*>(scratch + 40);
+    uint64_t* empty_bar = full_bar + S::kStages;
+    int* notes = reinterpret_cast<int*>(empty_bar + S::kStages);  // [stage]: keys of the tile that there are, and which of its halves were fetched
+
+    const int warp = __shfl_sync(kFullMask, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::kStages; ++s) {
+            mbar_init(&full_bar[s], 1);
+            mbar_init(&empty_bar[s], S::kComputeWarps);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
     pdl_trigger();
     pdl_wait();
 
-    long long total = 0, before = 0, tile = 0, tile_end = 0;
+    long long total = 0, before = 0;
     int unit = 0, ctas = 0;
     find_unit<S::kQueries>(a, scratch, [&](long long sum) {
         ctas = max(1, ctas_of(sum, a.grid));
         return static_cast<int>(blockIdx.x) < ctas ? first_tile(sum, blockIdx.x, ctas) : sum;
     }, total, unit, before);
     if (unit < 0) return;  // (more CTAs than tiles)
-    tile = first_tile(total, blockIdx.x, ctas);
-    tile_end = first_tile(total, blockIdx.x + 1, ctas);
-
-    Segment g;
-    g.unit = unit;
-    g.limit = unit_limit<S::kQueries>(a, unit);
-    g.tiles = (g.limit + kTileKeys - 1) / kTileKeys;
+    Run<S::kQueries> run;
+    Segment& g = run.g;
     {
-        const long long within = tile - before * a.cache.n_kv;
+        const long long first = first_tile(total, blockIdx.x, ctas), within = first - before * a.cache.n_kv;
+        run.left = first_tile(total, blockIdx.x + 1, ctas) - first;
+        g.unit = unit;
+        run.open(a);
         g.head = static_cast<int>(within / g.tiles);
         g.tile0 = static_cast<int>(within - static_cast<long long>(g.head) * g.tiles);
+        run.close();
+    }
+    __syncthreads();  // (barriers are there for all)
+    uint32_t limit = kSpinLimit;  // of every wait; one that has run out leaves one try to the others, and the CTA ends with its error noted
+
+    if (warp == S::kComputeWarps) {
+        // ---- the tiles of the whole run, through the ring: halves of 32 keys, which lie in one page each ----
+        const bool leader = elect_one();
+        int stage = 0, use = 0;
+        do {
+            const int b = g.unit / a.blocks;
+            const int32_t* pages = a.cache.table + static_cast<size_t>(b) * a.cache.width;
+            for (int t = g.tile0; t < g.tile1; ++t) {
+                int page[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int key = t * kTileKeys + 32 * h;
+                    page[h] = key < g.limit ? pages[key >> a.cache.page_shift] : -1;
+                    if (page[h] >= a.cache.pages) page[h] = -1;
+                }
+                if (use > 0 && !mbar_wait_warp(&empty_bar[stage], (use - 1) & 1, limit)) limit = 1;
+                if (leader) {
+                    const int halves = (page[0] >= 0 ? 1 : 0) + (page[1] >= 0 ? 1 : 0);
+                    notes[stage] = min(kTileKeys, g.limit - t * kTileKeys) | (page[0] >= 0 ? 256 : 0) | (page[1] >= 0 ? 512 : 0);
+                    mbar_expect_tx(&full_bar[stage], halves * (S::kStageBytes + S::kScaleBytes) / 2);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (page[h] < 0) continue;
+                        const int slot = (t * kTileKeys + 32 * h) & ((1 << a.cache.page_shift) - 1);
+#pragma unroll
+                        for (int which = 0; which < 2; ++which) {
+                            const int plane = (page[h] * 2 + which) * a.cache.n_kv + g.head;
+                            uint8_t* to = ring + stage * S::kStageBytes + which * S::kOperandBytes + h * 32 * S::kBoxBytes;
+#pragma unroll
+                            for (int box = 0; box < S::kBoxes; ++box)
+                                load_box(to + box * (kTileKeys * 128), &map, box * (S::kEight ? 128 : 64), slot, plane, &full_bar[stage]);
+                            if constexpr (S::kEight)
+                                load_bulk(ring_scales + (stage * 2 + which) * kTileKeys + 32 * h,
+                                          a.scales + (static_cast<long long>(plane) << a.cache.page_shift) + slot, 128, &full_bar[stage]);
+                        }
+                    }
+                }
+                __syncwarp();
+                if (++stage == S::kStages) { stage = 0; ++use; }
+            }
+        } while (run.next(a));
+        if (limit != kSpinLimit) {  // nothing may still be on its way when the CTA leaves
+            for (int s = 0; s < S::kStages; ++s) {
+                mbar_wait(&full_bar[s], 0, 1 << 14);
+                mbar_wait(&full_bar[s], 1, 1 << 14);
+            }
+            if (lane == 0) atomicCAS(&g_paged_error, 0, 1);
+        }
+        return;
     }
 
-    while (true) {
-        g.tile1 = static_cast<int>(min(static_cast<long long>(g.tiles), g.tile0 + (tile_end - tile)));
+    const int mt = warp % MT, group = warp / MT;
+    const int r0 = lane >> 2, c = lane & 3;
+    constexpr int kCompute = 32 * S::kComputeWarps;
+    int stage = 0, use = 0;
+    do {
         const int b = g.unit / a.blocks, block = g.unit - b * a.blocks;
         const int length = a.lengths[b];
-
-        // ---- a stage: 64 rows of K and of V, with their scales ----
-        const auto fetch = [&](int t, int stage) {
-            uint8_t* to = ring + stage * S::kStageBytes;
-            const uint32_t base = shared_u32(to);
-#pragma unroll
-            for (int i = threadIdx.x; i < 2 * kTileKeys * S::kChunks; i += S::kThreads) {
-                const int which = i / (kTileKeys * S::kChunks), rest = i - which * (kTileKeys * S::kChunks);
-                const int r = rest / S::kChunks, chunk = rest - r * S::kChunks, key = t * kTileKeys + r;
-                const long long at = key < g.limit ? a.cache.row(b, which, g.head, key) : -1;
-                copy16(base + which * (kTileKeys * S::kRowBytes) + S::place(r, chunk),
-                       static_cast<const uint8_t*>(a.pool) + (at < 0 ? 0 : at * S::kRowBytes + chunk * 16), at >= 0);
-            }
-            if constexpr (S::kEight) {
-                for (int i = threadIdx.x; i < 2 * kTileKeys; i += S::kThreads) {
-                    const int which = i / kTileKeys, r = i - which * kTileKeys, key = t * kTileKeys + r;
-                    const long long at = key < g.limit ? a.cache.row(b, which, g.head, key) : -1;
-                    copy4(base + 2 * kTileKeys * S::kRowBytes + i * 4, a.scales + (at < 0 ? 0 : at), at >= 0);
-                }
-            } else {
-                // (whether a row is there, where there are no scales to say so)
-                for (int i = threadIdx.x; i < kTileKeys; i += S::kThreads) {
-                    const int key = t * kTileKeys + i;
-                    const bool there = key < g.limit && a.cache.row(b, 0, g.head, key) >= 0;
-                    *reinterpret_cast<float*>(to + 2 * kTileKeys * S::kRowBytes + i * 4) = there ? 1.0f : 0.0f;
-                }
-            }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        };
-        __syncthreads();  // the ring and the queries of the segment before are done with
-#pragma unroll
-        for (int s = 0; s < S::kStages - 1; ++s) {
-            if (g.tile0 + s < g.tile1) fetch(g.tile0 + s, s);
-            else asm volatile("cp.async.commit_group;" ::: "memory");
-        }
 
         // ---- the block's queries, in the order in which the products take them ----
         // Lane c of a quad reads dims E (4 i + c) + 4 s .. + 3 of a key row (E elements to 16 bytes), so step E/4 i + s of the
         // product takes the same dims of the query.  fp16 rows are brought to a largest magnitude in [1, 2) by a power of two.
         constexpr int E = 16 / (S::kRowBytes / D), kPerChunk = E / 4;
-        for (int row = warp; row < S::kQueries; row += S::kThreads / 32) {
+        for (int row = warp; row < S::kQueries; row += S::kComputeWarps) {
             const int query = block * S::kQueries + row, i = query / a.group;
             const bool there = i < a.rows;
             float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -313,6 +396,7 @@ paged_attention_kernel(const __grid_constant__ AttnArgs a) {
             }
             if (lane == 0) q_factor[row] = back * a.scale * kLog2e;
         }
+        compute_sync<kCompute>();
 
         // positions of this thread's two queries; one that does not exist sees nothing
         int seen[2];
@@ -322,6 +406,7 @@ paged_attention_kernel(const __grid_constant__ AttnArgs a) {
             seen[h] = i < a.rows ? static_cast<int>(max(-1ll, static_cast<long long>(length) - a.rows + i)) : -1;
         }
         const int seen_by_all = static_cast<int>(max(-1ll, static_cast<long long>(length) - a.rows + min(a.rows - 1, block * S::kQueries / a.group)));
+        const float factor[2] = {q_factor[mt * 16 + r0], q_factor[mt * 16 + r0 + 8]};
 
         float o[D / 8][4], top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f};
 #pragma unroll
@@ -329,50 +414,52 @@ paged_attention_kernel(const __grid_constant__ AttnArgs a) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[n][j] = 0.0f;
 
-        int stage = 0;
         for (int t = g.tile0; t < g.tile1; ++t) {
-            asm volatile("cp.async.wait_group %0;" ::"n"(S::kStages - 2) : "memory");
-            __syncthreads();
-            {
-                const int next = t + S::kStages - 1;
-                if (next < g.tile1) fetch(next, stage == 0 ? S::kStages - 1 : stage - 1);
-                else asm volatile("cp.async.commit_group;" ::: "memory");
-            }
+            if (!mbar_wait_warp(&full_bar[stage], use & 1, limit)) limit = 1;
             const uint8_t* keys = ring + stage * S::kStageBytes;
-            const uint8_t* values = keys + kTileKeys * S::kRowBytes;
-            const float* consts = reinterpret_cast<const float*>(keys + 2 * kTileKeys * S::kRowBytes);
-            if (++stage == S::kStages) stage = 0;
+            uint8_t* values = ring + stage * S::kStageBytes + S::kOperandBytes;
+            const float* consts = ring_scales + stage * 2 * kTileKeys;
+            const int note = notes[stage];
+            // keys of this warp's sixteen that there are (they lie in one half of the tile)
+            const int there = note & (group >= kGroups / 2 ? 512 : 256) ? max(0, min(16, (note & 255) - 16 * group)) : 0;
+            const int first_key = t * kTileKeys + group * 16;
 
-            // A weight of zero does not hide a V row that is no number from the product, so rows that some of the block's queries
-            // see and others do not are looked at first: one with such a value is taken out and told to those who see it.
-            const bool hidden = KV != SPEC_DTYPE_INT8 && (t + 1) * kTileKeys > seen_by_all + 1 && seen_by_all + 1 < g.limit;
-            if (hidden) {
-                uint8_t* rows_v = ring + (stage == 0 ? S::kStages - 1 : stage - 1) * S::kStageBytes + kTileKeys * S::kRowBytes;
-                for (int i = threadIdx.x; i < kTileKeys; i += S::kThreads) bad[i] = 0;
-                __syncthreads();
-                for (int i = threadIdx.x; i < kTileKeys * S::kChunks; i += S::kThreads)
-                    if (not_numbers<KV>(*reinterpret_cast<const uint4*>(rows_v + i * 16))) bad[i / S::kChunks] = 1;
-                __syncthreads();
-                for (int i = threadIdx.x; i < kTileKeys * S::kChunks; i += S::kThreads)
-                    if (bad[i / S::kChunks]) *reinterpret_cast<uint4*>(rows_v + i * 16) = make_uint4(0u, 0u, 0u, 0u);
-                __syncthreads();
+            // A weight of zero does not hide a V row that is no number from the product.  Rows that are not there (left from
+            // before, or of other sequences) are cleared; rows that some of the block's queries see and others do not are looked at,
+            // and one with such a value is taken out and told to those who see it.
+            const bool hidden = KV != SPEC_DTYPE_INT8 && first_key + 15 > seen_by_all && seen_by_all + 1 < g.limit;
+            uint32_t bad = 0u;  // a bit per key
+            if (KV != SPEC_DTYPE_INT8 && (there < 16 || hidden)) {
+                if (hidden) {
+                    for (int i = lane; i < 16 * S::kChunks; i += 32) {
+                        const int r = i / S::kChunks;
+                        if (r < there && not_numbers<KV>(*reinterpret_cast<const uint4*>(values + S::place(group * 16 + r, i % S::kChunks)))) bad |= 1u << r;
+                    }
+                    bad = __reduce_or_sync(kFullMask, bad);
+                    // (the warps with the same keys look before one of them clears)
+                    if constexpr (MT > 1) asm volatile("bar.sync %0, %1;" ::"r"(2 + group), "n"(32 * MT) : "memory");
+                }
+                for (int i = lane; i < 16 * S::kChunks; i += 32) {
+                    const int r = i / S::kChunks;
+                    if (r >= there || (bad >> r & 1u)) *reinterpret_cast<uint4*>(values + S::place(group * 16 + r, i % S::kChunks)) = make_uint4(0u, 0u, 0u, 0u);
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // (before the next copy into this stage)
             }
-
-            // what each of this warp's 16 keys brings: (factor of the product, exponent added, factor of the sum)
+            // what each of the sixteen brings: (factor of the product, exponent added, factor of the sum)
             float4* mine = key_consts + warp * 16;
             __syncwarp();
             if (lane < 16) {
-                const int key = group * 16 + lane;
-                float4 k;
-                if constexpr (S::kEight) {
-                    const float sk = consts[key], sv = consts[kTileKeys + key];
-                    const bool there = sk != 0.0f;  // (no row's scale is zero; a row that is not there was filled with zeros)
-                    const bool number = magnitude(sv) < 0x7f800000u;  // (a row of V that is none makes the exponent none for who sees it, and no one else's sum)
-                    k = make_float4(sk, !there ? -INFINITY : number ? __log2f(sv) : NAN, there && number ? __fdividef(1.0f, sv) : 0.0f, 0.0f);
-                } else {
-                    k = make_float4(1.0f, consts[key] != 0.0f ? 0.0f : -INFINITY, 1.0f, 0.0f);
+                float4 k = make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
+                if (lane < there) {
+                    if constexpr (S::kEight) {
+                        const float sk = consts[group * 16 + lane], sv = consts[kTileKeys + group * 16 + lane];
+                        // (a row of V that is no number makes the exponent none for who sees it, and no one else's sum)
+                        k = magnitude(sv) < 0x7f800000u ? make_float4(sk, __log2f(sv), __fdividef(1.0f, sv), 0.0f) : make_float4(sk, NAN, 0.0f, 0.0f);
+                    } else {
+                        k = make_float4(1.0f, 0.0f, 1.0f, 0.0f);
+                    }
+                    if (bad >> lane & 1u) k.y = NAN;
                 }
-                if (hidden && bad[key]) k.y = NAN;
                 mine[lane] = k;
             }
             __syncwarp();
@@ -403,8 +490,7 @@ paged_attention_kernel(const __grid_constant__ AttnArgs a) {
                 }
             }
             // ---- exponents, their running maximum, weights ----
-            const float factor[2] = {q_factor[mt * 16 + r0], q_factor[mt * 16 + r0 + 8]};
-            const bool masked = t * kTileKeys + group * 16 + 15 > seen_by_all;
+            const bool masked = first_key + 15 > seen_by_all;
             float inv[2][2];
             float now[2] = {-INFINITY, -INFINITY};
 #pragma unroll
@@ -417,7 +503,7 @@ paged_attention_kernel(const __grid_constant__ AttnArgs a) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         float e = fmaf(s[n][2 * h + x], k.x * factor[h], k.y);
-                        if (k.y == -INFINITY || (masked && t * kTileKeys + group * 16 + key > seen[h])) e = -INFINITY;
+                        if (k.y == -INFINITY || (masked && first_key + key > seen[h])) e = -INFINITY;
                         s[n][2 * h + x] = e;
                         now[h] = fmaxf(now[h], e);
                     }
@@ -460,7 +546,7 @@ paged_attention_kernel(const __grid_constant__ AttnArgs a) {
                 p.w = pack2<S::kBf16>(s[1][2], s[1][3]);
             }
             // ---- weights times values: key 2 c, 2 c + 1 (and + 8) of the product are the columns of the scores ----
-            const uint32_t v_base = shared_u32(values);
+            const uint32_t v_base = smem_u32(values);
             const int v_row = group * 16 + ((lane >> 3) & 1) * 8 + S::key_of(lane & 7);
 #pragma unroll
             for (int i = 0; i < S::kChunks / 2; ++i) {
@@ -479,18 +565,19 @@ paged_attention_kernel(const __grid_constant__ AttnArgs a) {
                     }
                 }
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&empty_bar[stage]);
+            if (++stage == S::kStages) { stage = 0; ++use; }
         }
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             sum[h] += __shfl_xor_sync(kFullMask, sum[h], 1);
             sum[h] += __shfl_xor_sync(kFullMask, sum[h], 2);
         }
         // ---- the four groups' states become one: groups 2, 3 into 0, 1, then 1 into 0 ----
-        float* merge = reinterpret_cast<float*>(ring);
 #pragma unroll
         for (int step = kGroups / 2; step > 0; step >>= 1) {
-            __syncthreads();
+            compute_sync<kCompute>();  // (whoever read the place before is done)
             if (group >= step && group < 2 * step) {
                 float* to = merge + ((group - step) * MT + mt) * 16 * (D + 2) + lane;
 #pragma unroll
@@ -505,7 +592,7 @@ paged_attention_kernel(const __grid_constant__ AttnArgs a) {
                     ml[16 + r0 + 8] = sum[1];
                 }
             }
-            __syncthreads();
+            compute_sync<kCompute>();
             if (group < step) {
                 const float* from = merge + (group * MT + mt) * 16 * (D + 2);
                 float keep[2], take[2];
@@ -556,19 +643,9 @@ paged_attention_kernel(const __grid_constant__ AttnArgs a) {
                 }
             }
         }
-        // ---- the next segment of the run ----
-        tile += g.tile1 - g.tile0;
-        if (tile >= tile_end) return;
-        g.tile0 = 0;
-        if (++g.head == a.cache.n_kv) {
-            g.head = 0;
-            do {
-                ++g.unit;
-                g.limit = unit_limit<S::kQueries>(a, g.unit);
-            } while (g.limit == 0);
-            g.tiles = (g.limit + kTileKeys - 1) / kTileKeys;
-        }
-    }
+        compute_sync<kCompute>();  // (the queries' place is free for the next segment's)
+    } while (run.next(a));
+    if (limit != kSpinLimit && lane == 0) atomicCAS(&g_paged_error, 0, 2);
 }
 
 // Joins the states of a segment that several CTAs had, in their order; a segment without a key gets its zeros here.  A warp per
@@ -641,13 +718,22 @@ join_kernel(const __grid_constant__ AttnArgs a) {
     }
 }
 
-// 16-query tiles of a block: as many as the queries of a (sequence, KV head) fill, at most four.
-int query_tiles(int rows, int group) {
-    const long long queries = static_cast<long long>(rows) * group;
-    return queries <= 16 ? 1 : queries <= 32 ? 2 : 4;
-}
+// 16-query tiles of a block: two where the queries of a (sequence, KV head) are more than sixteen.  (Four do not fit: sixteen
+// warps and the one that fetches leave 96 registers to a thread, and 64 of them are the weighted sum.)
+int query_tiles(int rows, int group) { return static_cast<long long>(rows) * group <= 16 ? 1 : 2; }
 
 size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
+
+// The pool as planes [page, K or V, head] of page_size rows, fetched in boxes of 32 rows (128 bytes of each, or the whole row).
+int rows_map(const AttnArgs& a, bool eight, int d, int box_bytes, CUtensorMap* out) {
+    const int bytes = eight ? 1 : 2;
+    const unsigned long long page = 1ull << a.cache.page_shift, planes = 2ull * a.cache.pages * a.cache.n_kv;
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(d), page, planes};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(d) * bytes, page * d * bytes};
+    const cuuint32_t box[3] = {static_cast<cuuint32_t>(box_bytes / bytes), 32, 1};
+    return encode_map(eight ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 3, a.pool, dims, strides, box,
+                      box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, out);
+}
 
 template <int D, int KV, int MT>
 int launch(const AttnArgs& args, cudaStream_t stream) {
@@ -656,17 +742,18 @@ int launch(const AttnArgs& args, cudaStream_t stream) {
     int status = allow_shared_memory(configured, paged_attention_kernel<D, KV, MT>, S::kSmem);
     if (status != SPEC_OK) return status;
     AttnArgs a = args;
-    constexpr int per_sm = MT == 1 ? 3 : 1;
-    a.grid = 148 * per_sm;
-    status = launch_pdl(paged_attention_kernel<D, KV, MT>, dim3(a.grid), dim3(S::kThreads), S::kSmem, stream, a);
+    a.grid = 148 * S::kPerSm;
+    CUtensorMap map;
+    status = rows_map(a, S::kEight, D, S::kBoxBytes, &map);
+    if (status != SPEC_OK) return status;
+    status = launch_pdl(paged_attention_kernel<D, KV, MT>, dim3(a.grid), dim3(S::kThreads), S::kSmem, stream, map, a);
     if (status != SPEC_OK) return status;
     return launch_pdl(join_kernel<D, S::kQueries>, dim3(a.units * a.cache.n_kv, S::kQueries / 4), dim3(128), 0, stream, a);
 }
 
 template <int D, int KV>
 int launch_tiles(const AttnArgs& a, cudaStream_t stream) {
-    const int mt = query_tiles(a.rows, a.group);
-    return mt == 1 ? launch<D, KV, 1>(a, stream) : mt == 2 ? launch<D, KV, 2>(a, stream) : launch<D, KV, 4>(a, stream);
+    return query_tiles(a.rows, a.group) == 1 ? launch<D, KV, 1>(a, stream) : launch<D, KV, 2>(a, stream);
 }
 
 template <int D>
@@ -686,6 +773,14 @@ bool fits(int batch, int rows, int n_heads, int n_kv_heads, int d_head) {
 long long units_of(int batch, int rows, int group, int queries) { return static_cast<long long>(batch) * ((static_cast<long long>(rows) * group + queries - 1) / queries); }
 
 }  // namespace
+
+int paged_attention_take_error() {
+    int v = 0, zero = 0;
+    if (cudaMemcpyFromSymbol(&v, g_paged_error, sizeof(int)) != cudaSuccess) return -1;
+    if (v) cudaMemcpyToSymbol(g_paged_error, &zero, sizeof(int));
+    return v;
+}
+
 }  // namespace spec
 
 extern "C" size_t spec_paged_attention_workspace_bytes(int batch, int rows, int n_heads, int n_kv_heads, int d_head) {
@@ -713,6 +808,8 @@ extern "C" int spec_paged_attention(const void* q, int dtype, int64_t q_stride, 
     if (!q || !out || !lengths) return fail(SPEC_ERR_BAD_ARG, "%s: null pointer", who);
     if (!aligned_to(q, 8) || !aligned_to(out, 8) || q_stride % 4 || !aligned_to(lengths, 4)) return fail(SPEC_ERR_BAD_ARG, "%s: q and out have to start on 8 bytes, q's rows too", who);
     if (q_stride < static_cast<int64_t>(n_heads) * d_head) return fail(SPEC_ERR_BAD_ARG, "%s: q's row stride is below the heads' elements", who);
+    if (scales && !aligned_to(scales, 16)) return fail(SPEC_ERR_BAD_ARG, "%s: scales have to start on 16 bytes", who);
+    if (static_cast<long long>(pages) * 2 * n_kv_heads > 0x7fffffffll) return fail(SPEC_ERR_BAD_ARG, "%s: pages=%d", who, pages);
     a.group = n_heads / n_kv_heads;
     const int queries = 16 * query_tiles(rows, a.group);
     const long long units = units_of(batch, rows, a.group, queries);

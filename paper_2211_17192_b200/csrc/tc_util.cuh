@@ -92,5 +92,8 @@ __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.
 // A tensor map over a bf16 matrix [rows, cols] row-major, fetched in boxes of [box_rows, 64], with the 128-byte swizzle
 // applied on the way in unless the data is stored swizzled already; cached by its arguments.  gemm_tc.cu
 int cached_bf16_map(const void* base, int rows, int cols, int box_rows, bool swizzle, CUtensorMap* out);
+// Any tensor map without interleaving, zeros past its edges, encoded anew (under a microsecond; nothing is kept by address).
+int encode_map(CUtensorMapDataType type, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box,
+               CUtensorMapSwizzle swizzle, CUtensorMap* out);
 
 }  // namespace spec
