@@ -103,6 +103,23 @@ __device__ __forceinline__ void widen(uint32_t codes, uint32_t& first, uint32_t&
     }
 }
 
+// The hardware's approximations, subnormal results as zeros: 2^x to two units of the last place, log2 to 2^-22, 1/x to one unit.
+__device__ __forceinline__ float exp2_of(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float log2_of(float x) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float reciprocal_of(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 // Whether a NaN or an infinity is among 16 bytes of a row.
 template <int KV>
 __device__ __forceinline__ bool not_numbers(const uint4& v) {
@@ -208,7 +225,7 @@ struct Shape {
     static constexpr int kQueryBytes = kQueries * D * 2;
     static constexpr int kMerge = 2 * MT * 16 * (D + 2) * 4;  // two groups' states
     static constexpr int kPerSm = MT == 1 ? (kRowBytes <= 128 ? 3 : 2) : 1;
-    static constexpr int kFixed = kMerge + kQueryBytes + kQueries * 4 + 40 * 8 + kComputeWarps * 16 * 16 + 1024 /* alignment */ + 256 /* barriers, notes */;
+    static constexpr int kFixed = kMerge + kQueryBytes + kQueries * 4 + 40 * 8 + 1024 /* alignment */ + 256 /* barriers, notes */;
     static constexpr int kStagesThatFit = ((227 * 1024 + 1024) / kPerSm - 1024 - kFixed) / (kStageBytes + kScaleBytes);
     static constexpr int kStages = kStagesThatFit < 8 ? kStagesThatFit : 8;
     static constexpr int kSmem = kStages * (kStageBytes + kScaleBytes) + kFixed;
@@ -262,8 +279,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
     float* ring_scales = reinterpret_cast<float*>(ring + S::kStages * S::kStageBytes);  // [stage][K, V][64]
     float* merge = reinterpret_cast<float*>(ring + S::kStages * (S::kStageBytes + S::kScaleBytes));
     uint4* q_frag = reinterpret_cast<uint4*>(merge + S::kMerge / 4);                 // [MT][D / 16][32 lanes]
-    float4* key_consts = reinterpret_cast<float4*>(q_frag + S::kQueryBytes / 16);                               // [warp][16 keys]
-    float* q_factor = reinterpret_cast<float*>(key_consts + S::kComputeWarps * 16);  // what a row's products are multiplied with
+    float* q_factor = reinterpret_cast<float*>(q_frag + S::kQueryBytes / 16);  // what a row's products are multiplied with
     long long* scratch = reinterpret_cast<long long*>(q_factor + S::kQueries);
     uint64_t* full_bar = reinterpret_cast<uint64_t*>(scratch + 40);
     uint64_t* empty_bar = full_bar + S::kStages;
@@ -445,25 +461,6 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // (before the next copy into this stage)
             }
-            // what each of the sixteen brings: (factor of the product, exponent added, factor of the sum)
-            float4* mine = key_consts + warp * 16;
-            __syncwarp();
-            if (lane < 16) {
-                float4 k = make_float4(0.0f, -INFINITY, 0.0f, 0.0f);
-                if (lane < there) {
-                    if constexpr (S::kEight) {
-                        const float sk = consts[group * 16 + lane], sv = consts[kTileKeys + group * 16 + lane];
-                        // (a row of V that is no number makes the exponent none for who sees it, and no one else's sum)
-                        k = magnitude(sv) < 0x7f800000u ? make_float4(sk, __log2f(sv), __fdividef(1.0f, sv), 0.0f) : make_float4(sk, NAN, 0.0f, 0.0f);
-                    } else {
-                        k = make_float4(1.0f, 0.0f, 1.0f, 0.0f);
-                    }
-                    if (bad >> lane & 1u) k.y = NAN;
-                }
-                mine[lane] = k;
-            }
-            __syncwarp();
-
             float s[2][4];
 #pragma unroll
             for (int n = 0; n < 2; ++n)
@@ -490,24 +487,44 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                 }
             }
             // ---- exponents, their running maximum, weights ----
-            const bool masked = first_key + 15 > seen_by_all;
             float inv[2][2];
             float now[2] = {-INFINITY, -INFINITY};
 #pragma unroll
             for (int n = 0; n < 2; ++n)
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    const int key = n * 8 + S::key_of(2 * c + x);
-                    const float4 k = mine[key];
-                    inv[n][x] = k.z;
+                    inv[n][x] = 1.0f;
+                    if constexpr (S::kEight) {
+                        const int key = group * 16 + n * 8 + S::key_of(2 * c + x);
+                        const float sk = consts[key], sv = consts[kTileKeys + key], raise = log2_of(sv);
+                        inv[n][x] = reciprocal_of(sv);
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        float e = fmaf(s[n][2 * h + x], k.x * factor[h], k.y);
-                        if (k.y == -INFINITY || (masked && first_key + key > seen[h])) e = -INFINITY;
-                        s[n][2 * h + x] = e;
-                        now[h] = fmaxf(now[h], e);
+                        for (int h = 0; h < 2; ++h) s[n][2 * h + x] = fmaf(s[n][2 * h + x], sk * factor[h], raise);
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) s[n][2 * h + x] *= factor[h];
                     }
                 }
+            if (there < 16 || first_key + 15 > seen_by_all) {  // keys that are not there, or not for every query
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int key = n * 8 + S::key_of(2 * c + x);
+                        bool number = !(bad >> key & 1u);
+                        if constexpr (S::kEight) number = number && magnitude(consts[kTileKeys + group * 16 + key]) < 0x7f800000u;
+                        // (a row of V that is no number makes the exponent none for who sees it, and no one else's sum)
+                        if (!number || key >= there) inv[n][x] = 0.0f;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            float& e = s[n][2 * h + x];
+                            if (!number) e = NAN;
+                            if (key >= there || first_key + key > seen[h]) e = -INFINITY;
+                        }
+                    }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) now[h] = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 now[h] = fmaxf(now[h], __shfl_xor_sync(kFullMask, now[h], 1));
@@ -518,7 +535,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const float higher = fmaxf(top[h], now[h]);
-                    shrink[h] = top[h] == -INFINITY ? 0.0f : exp2f(top[h] - higher);
+                    shrink[h] = top[h] == -INFINITY ? 0.0f : exp2_of(top[h] - higher);
                     top[h] = higher;
                     sum[h] *= shrink[h];
                 }
@@ -537,7 +554,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                 for (int n = 0; n < 2; ++n)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        s[n][j] = exp2f(s[n][j] - from[j >> 1]);
+                        s[n][j] = exp2_of(s[n][j] - from[j >> 1]);
                         sum[j >> 1] = fmaf(s[n][j], inv[n][j & 1], sum[j >> 1]);
                     }
                 p.x = pack2<S::kBf16>(s[0][0], s[0][1]);
@@ -599,8 +616,8 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const float other = from[16 * D + r0 + 8 * h], higher = fmaxf(top[h], other);
-                    keep[h] = top[h] == -INFINITY ? 0.0f : exp2f(top[h] - higher);
-                    take[h] = other == -INFINITY ? 0.0f : exp2f(other - higher);
+                    keep[h] = top[h] == -INFINITY ? 0.0f : exp2_of(top[h] - higher);
+                    take[h] = other == -INFINITY ? 0.0f : exp2_of(other - higher);
                     sum[h] = sum[h] * keep[h] + from[16 * D + 16 + r0 + 8 * h] * take[h];
                     top[h] = higher;
                 }
@@ -701,7 +718,7 @@ join_kernel(const __grid_constant__ AttnArgs a) {
 #pragma unroll 4
         for (int p = first; p <= last; ++p) {
             const float2 ml = a.partial_ml[(slot0 + p) * QT + row];
-            const float w = ml.x == -INFINITY ? 0.0f : exp2f(ml.x - top);
+            const float w = ml.x == -INFINITY ? 0.0f : exp2_of(ml.x - top);
             sum = fmaf(w, ml.y, sum);
             const float* part = a.partial + ((slot0 + p) * QT + row) * D + kPer * lane;
 #pragma unroll
