@@ -293,8 +293,8 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    pdl_trigger();
     pdl_wait();
+    pdl_trigger();  // (behind the wait: the joining kernel reads the lengths ahead of its own)
 
     long long total = 0, before = 0;
     int unit = 0, ctas = 0;
@@ -665,23 +665,27 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
     if (limit != kSpinLimit && lane == 0) atomicCAS(&g_paged_error, 0, 2);
 }
 
-// Joins the states of a segment that several CTAs had, in their order; a segment without a key gets its zeros here.  A warp per
-// query, grid = (segments, queries of a block / 4).
-template <int D, int QT>
+// Joins the states of a segment that several CTAs had, in their order; a segment without a key gets its zeros here.  SHARE warps of
+// a CTA have one query: they take its pieces in turn, eight at a time with all their loads in flight.  Where segments are few, and
+// have many pieces, four warps to a query (17 pieces, one after the other in a warp: 14.6 us for the whole call, so 11.6), else one
+// (384 segments of seven queries: 37 us for the whole call, 40 with four).
+template <int D, int QT, int SHARE>
 __global__ void __launch_bounds__(128)
 join_kernel(const __grid_constant__ AttnArgs a) {
-    __shared__ long long scratch[40];
+    constexpr int kPer = D / 32, kBatch = 8, kWarps = 4;
+    __shared__ long long counts[2 * kWarps];
+    __shared__ float states[SHARE][D + 2];
     pdl_trigger();
-    pdl_wait();
     const int unit = blockIdx.x / a.cache.n_kv, head = blockIdx.x - unit * a.cache.n_kv;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int b = unit / a.blocks, block = unit - b * a.blocks;
-    const int row = blockIdx.y * 4 + warp, query = block * QT + row, i = query / a.group;
+    const int row = blockIdx.y * (kWarps / SHARE) + warp / SHARE, query = block * QT + row, i = query / a.group;
+    // (the lengths may be read ahead of the wait: the kernel in front lets this one start behind its own wait only)
     const int limit = unit_limit<QT>(a, unit), tiles = (limit + kTileKeys - 1) / kTileKeys;
     long long total = 0, front = 0;
     {  // tiles of all units, and of those before this one
         long long all = 0, mine = 0;
-        for (int u = threadIdx.x; u < a.units; u += 128) {
+        for (int u = threadIdx.x; u < a.units; u += 32 * kWarps) {
             const int n = (unit_limit<QT>(a, u) + kTileKeys - 1) / kTileKeys;
             all += n;
             if (u < unit) mine += n;
@@ -692,44 +696,83 @@ join_kernel(const __grid_constant__ AttnArgs a) {
             mine += __shfl_xor_sync(kFullMask, mine, o);
         }
         if (lane == 0) {
-            scratch[warp] = all;
-            scratch[4 + warp] = mine;
+            counts[warp] = all;
+            counts[kWarps + warp] = mine;
         }
         __syncthreads();
-        for (int w = 0; w < 4; ++w) {
-            total += scratch[w];
-            front += scratch[4 + w];
+        for (int w = 0; w < kWarps; ++w) {
+            total += counts[w];
+            front += counts[kWarps + w];
         }
         total *= a.cache.n_kv;
         front = front * a.cache.n_kv + static_cast<long long>(head) * tiles;
     }
-    if (i >= a.rows) return;
+    if (row >= QT || i >= a.rows) return;
+    pdl_wait();
     const size_t at = ((static_cast<size_t>(b) * a.rows + i) * a.n_heads + head * a.group + query - i * a.group) * D;
-    constexpr int kPer = D / 32;
-    float v[kPer] = {};
+    float v[kPer] = {}, top = -INFINITY, sum = 0.0f;
     if (tiles > 0) {
         const int ctas = ctas_of(total, a.grid), first = owner_of(total, front, ctas), last = owner_of(total, front + tiles - 1, ctas);
         if (first == last) return;  // (written by the CTA that had all of it)
         const long long slot0 = static_cast<long long>(unit) * a.cache.n_kv + head;
-        float top = -INFINITY;
-        for (int p = first + lane; p <= last; p += 32) top = fmaxf(top, a.partial_ml[(slot0 + p) * QT + row].x);
-        top = warp_max(top);
-        float sum = 0.0f;
-#pragma unroll 4
-        for (int p = first; p <= last; ++p) {
-            const float2 ml = a.partial_ml[(slot0 + p) * QT + row];
-            const float w = ml.x == -INFINITY ? 0.0f : exp2_of(ml.x - top);
-            sum = fmaf(w, ml.y, sum);
-            const float* part = a.partial + ((slot0 + p) * QT + row) * D + kPer * lane;
+        for (int p0 = first + warp % SHARE; p0 <= last; p0 += SHARE * kBatch) {
+            float2 ml[kBatch];
+            float part[kBatch][kPer];
 #pragma unroll
-            for (int j = 0; j < kPer; ++j) v[j] = fmaf(w, part[j], v[j]);
+            for (int k = 0; k < kBatch; ++k) {
+                const int p = p0 + k * SHARE;
+                ml[k] = make_float2(-INFINITY, 0.0f);
+                if (p <= last) {
+                    ml[k] = a.partial_ml[(slot0 + p) * QT + row];
+                    const float* from = a.partial + ((slot0 + p) * QT + row) * D + kPer * lane;
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j) part[k][j] = from[j];
+                }
+            }
+            float higher = top;
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) higher = fmaxf(higher, ml[k].x);
+            const float keep = top == -INFINITY ? 0.0f : exp2_of(top - higher);
+            sum *= keep;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) v[j] *= keep;
+            top = higher;
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                if (p0 + k * SHARE > last) continue;
+                const float w = ml[k].x == -INFINITY ? 0.0f : exp2_of(ml[k].x - top);
+                sum = fmaf(w, ml[k].y, sum);
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) v[j] = fmaf(w, part[k][j], v[j]);
+            }
         }
-        const float by = sum == 0.0f ? 0.0f : __fdividef(1.0f, sum);
+    }
+    if constexpr (SHARE > 1) {
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) v[j] *= by;
+        for (int j = 0; j < kPer; ++j) states[warp][kPer * lane + j] = v[j];
+        if (lane == 0) {
+            states[warp][D] = top;
+            states[warp][D + 1] = sum;
+        }
+        __syncthreads();
+        if (warp > 0) return;
+        top = -INFINITY;
+        sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) v[j] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < SHARE; ++k) top = fmaxf(top, states[k][D]);
+#pragma unroll
+        for (int k = 0; k < SHARE; ++k) {
+            const float w = states[k][D] == -INFINITY ? 0.0f : exp2_of(states[k][D] - top);
+            sum = fmaf(w, states[k][D + 1], sum);
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) v[j] = fmaf(w, states[k][kPer * lane + j], v[j]);
+        }
     }
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
+        if (sum != 0.0f) v[j] = __fdividef(v[j], sum);  // (a NaN stays; a row without a key has zeros)
         if (a.q_bf16) static_cast<__nv_bfloat16*>(a.out)[at + kPer * lane + j] = __float2bfloat16_rn(v[j]);
         else static_cast<__half*>(a.out)[at + kPer * lane + j] = __float2half_rn(v[j]);
     }
@@ -765,7 +808,9 @@ int launch(const AttnArgs& args, cudaStream_t stream) {
     if (status != SPEC_OK) return status;
     status = launch_pdl(paged_attention_kernel<D, KV, MT>, dim3(a.grid), dim3(S::kThreads), S::kSmem, stream, map, a);
     if (status != SPEC_OK) return status;
-    return launch_pdl(join_kernel<D, S::kQueries>, dim3(a.units * a.cache.n_kv, S::kQueries / 4), dim3(128), 0, stream, a);
+    const int segments = a.units * a.cache.n_kv, queries = static_cast<int>(std::min<long long>(S::kQueries, static_cast<long long>(a.rows) * a.group));
+    if (segments * 4 <= a.grid) return launch_pdl(join_kernel<D, S::kQueries, 4>, dim3(segments, queries), dim3(128), 0, stream, a);
+    return launch_pdl(join_kernel<D, S::kQueries, 1>, dim3(segments, (queries + 3) / 4), dim3(128), 0, stream, a);
 }
 
 template <int D, int KV>
