@@ -14,6 +14,7 @@
 // Every wait on an mbarrier is bounded; on expiry the kernel records an error code, waits (with a limit) for its copies and
 // leaves, tensor memory freed.
 #include <algorithm>
+#include <cstdlib>
 
 #include "fp8_util.cuh"
 #include "tc_util.cuh"
@@ -38,9 +39,9 @@ struct LinearArgs {
     const float *x_scales, *w_scales, *bias;
     const void* residual;
     void* y;
-    int rows, n_out, k_blocks, act, tokens /* rows of x per tile: the MMA's N */, stages, y_dtype;
-    uint32_t limit;
-    int drill;
+    int rows, n_out, k_blocks, act, tokens /* rows of x per tile: the MMA's N */, stages;
+    uint32_t limit;  // of every wait
+    int tiles, token_tiles;  // wide kernel: tiles of 256 rows of W by `tokens` rows of x, those of x neighbours
 };
 
 // e4m3 x e4m3 -> fp32, both operands K-major.
@@ -92,16 +93,8 @@ __device__ __forceinline__ void store_peer(uint32_t here, uint32_t rank, float v
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there), "f"(v) : "memory");
 }
 
-__device__ __forceinline__ float load_as_float(const void* p, int dtype, size_t i) {
-    if (dtype == SPEC_DTYPE_FP32) return static_cast<const float*>(p)[i];
-    if (dtype == SPEC_DTYPE_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
-    return __half2float(static_cast<const __half*>(p)[i]);
-}
-__device__ __forceinline__ void store_from_float(void* p, int dtype, size_t i, float v) {
-    if (dtype == SPEC_DTYPE_FP32) static_cast<float*>(p)[i] = v;
-    else if (dtype == SPEC_DTYPE_BF16) static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
-    else static_cast<__half*>(p)[i] = __float2half_rn(v);
-}
+// The columns that a CTA of a cluster finishes, from each of its CTAs.
+__host__ __device__ __forceinline__ int exchange_bytes(int tokens, int splits) { return splits > 1 ? splits * ((tokens + splits - 1) / splits) * kTileM * 4 : 0; }
 
 // What a lane of an epilogue warp knows of its accumulator lane (row of W), constant over a tile.
 struct LaneColumn {
@@ -119,32 +112,63 @@ __device__ __forceinline__ LaneColumn lane_column(const LinearArgs& a, int tile,
     c.column = in && !(gated && lane >= 16) ? f : -1;
     return c;
 }
-// One accumulator value per lane (a row r of x, 32 rows of W) to y.  Whole warps only.
-__device__ __forceinline__ void finish(const LinearArgs& a, const LaneColumn& c, int r, float acc) {
-    float z = acc * a.x_scales[r] * c.scale + c.bias;
-    if (a.act >= kActGatedGelu) {
-        const float up = __shfl_xor_sync(kFullMask, z, 16);
-        z = (a.act == kActGatedGelu ? gelu_tanh(z) : silu(z)) * up;
-    } else if (a.act == kActGelu) {
-        z = gelu_tanh(z);
+// x * sigmoid(s): with s = x this is silu, with s = 2 sqrt(2 / pi) (x + 0.044715 x^3) it is x (1 + tanh(s / 2)) / 2, the tanh form of
+// gelu.  From the hardware's 2^x and reciprocal: off by less than 2^-21 |x|.
+__device__ __forceinline__ float gate(float x, float s) { return __fdividef(x, 1.0f + __expf(-s)); }
+__device__ __forceinline__ float gelu_argument(float x) { return x * fmaf(0.0713548162726f * x, x, 1.5957691216057f); }
+
+// COLS neighbouring accumulator columns (rows r0 .. of x, `count` of them) of a warp's 32 rows of W to y.  Everything is loaded
+// before anything is stored: the loads are in flight together (one column after the other took 0.2 to 0.4 us each).
+template <typename T, int COLS>
+__device__ __forceinline__ void finish(const LinearArgs& a, const LaneColumn& c, int r0, int count, float (&z)[COLS]) {
+    float x_scale[COLS], add[COLS];
+    const float* scales = a.x_scales + r0;
+    const size_t at = static_cast<size_t>(r0) * a.n_out + (c.column < 0 ? 0 : c.column);
+    const T* residual = static_cast<const T*>(a.residual) + at;
+    T* y = static_cast<T*>(a.y) + at;
+#pragma unroll
+    for (int i = 0; i < COLS; ++i) x_scale[i] = i < count ? scales[i] : 0.0f;
+    if (a.residual) {
+#pragma unroll
+        for (int i = 0; i < COLS; ++i) add[i] = i < count && c.column >= 0 ? to_float(residual[static_cast<size_t>(i) * a.n_out]) : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < COLS; ++i) z[i] = fmaf(z[i] * x_scale[i], c.scale, c.bias);
+    if (a.act == kActGelu) {
+#pragma unroll
+        for (int i = 0; i < COLS; ++i) z[i] = gate(z[i], gelu_argument(z[i]));
     } else if (a.act == kActSilu) {
-        z = silu(z);
+#pragma unroll
+        for (int i = 0; i < COLS; ++i) z[i] = gate(z[i], z[i]);
+    } else if (a.act >= kActGatedGelu) {
+        // (both halves of the warp go through the function, so that the up half's lanes need no branch of their own)
+        const bool gelu = a.act == kActGatedGelu;
+#pragma unroll
+        for (int i = 0; i < COLS; ++i) {
+            const float up = __shfl_xor_sync(kFullMask, z[i], 16);
+            z[i] = gate(z[i], gelu ? gelu_argument(z[i]) : z[i]) * up;
+        }
     }
     if (c.column < 0) return;
-    const size_t at = static_cast<size_t>(r) * a.n_out + c.column;
-    if (a.residual) z += load_as_float(a.residual, a.y_dtype, at);
-    store_from_float(a.y, a.y_dtype, at, z);
+    if (a.residual) {
+#pragma unroll
+        for (int i = 0; i < COLS; ++i) z[i] += add[i];
+    }
+#pragma unroll
+    for (int i = 0; i < COLS; ++i)
+        if (i < count) y[static_cast<size_t>(i) * a.n_out] = from_float<T>(z[i]);
 }
 
 // grid = (tiles of 128 rows of W x CTAs of a cluster, tiles of x), clusters along x, block = kThreads.
+template <typename T>
 __global__ void __launch_bounds__(kThreads)
 linear_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ LinearArgs a) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const int stage_bytes = kTileBytes + a.tokens * kBlockK;
-    float* exchange = reinterpret_cast<float*>(smem + a.stages * stage_bytes);  // clusters of two and more: tokens * 128 floats
+    float* exchange = reinterpret_cast<float*>(smem + a.stages * stage_bytes);  // clusters of two and more: exchange_bytes() of them
     const uint32_t splits = cluster_size(), rank = cluster_rank();
-    uint64_t* full_bar = reinterpret_cast<uint64_t*>(smem + a.stages * stage_bytes + (splits > 1 ? a.tokens * kTileM * 4 : 0));
+    uint64_t* full_bar = reinterpret_cast<uint64_t*>(smem + a.stages * stage_bytes + exchange_bytes(a.tokens, splits));
     uint64_t* empty_bar = full_bar + kMaxStages;
     uint64_t* acc_bar = empty_bar + kMaxStages;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_bar + 1);
@@ -177,7 +201,7 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
     pdl_wait();
 
     if (warp == 0) {
-        const bool leader = elect_one() && !a.drill;
+        const bool leader = elect_one();
         const bool gated = a.act >= kActGatedGelu;
         int s = 0, use = 0;
         for (int kb = kb0; kb < kb1; ++kb) {
@@ -235,39 +259,45 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
     if (splits == 1) {
         if (reader && ok)
             for (int c0 = 0; c0 < valid; c0 += 16) {
-                uint32_t v[16];
-                tmem_ld16(acc + c0, v);
+                float z[16];
+                tmem_ld16(acc + c0, reinterpret_cast<uint32_t(&)[16]>(z));
                 tmem_ld_wait();
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (c0 + i < valid) finish(a, column, row0 + c0 + i, __uint_as_float(v[i]));
+                finish<T, 16>(a, column, row0 + c0, valid - c0, z);
             }
     } else {
-        // element (token c, quarter) is unit 4 c + quarter of 32 lanes; CTA r finishes units [first(r), first(r + 1))
-        const int units = 4 * valid, most = (units + splits - 1) / splits;
+        // CTA r finishes columns [r each, (r + 1) each): the others' sums of these lie in its exchange as [CTA][column][128]
+        const int each = (valid + splits - 1) / splits;
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // everyone is there
         if (reader && ok)
             for (int c0 = 0; c0 < valid; c0 += 16) {
                 uint32_t v[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] = 0u;
                 if (have) {
                     tmem_ld16(acc + c0, v);
                     tmem_ld_wait();
                 }
+                int to = c0 / each, within = c0 - to * each;
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
                     if (c0 + i < valid) {
-                        const int unit = 4 * (c0 + i) + quarter, to = unit / most;
-                        store_peer(smem_u32(exchange + (rank * most + unit - to * most) * 32 + lane), to, have ? __uint_as_float(v[i]) : 0.0f);
+                        store_peer(smem_u32(exchange + (rank * each + within) * kTileM + quarter * 32 + lane), to, __uint_as_float(v[i]));
+                        if (++within == each) { within = 0; ++to; }
                     }
             }
         cluster_sync_all();
         if (reader && ok) {
-            const int u0 = rank * most, u1 = min(units, u0 + most);
-            for (int unit = u0; unit < u1; ++unit) {
-                if ((unit & 3) != quarter) continue;
-                float sum = 0.0f;
-                for (uint32_t p = 0; p < splits; ++p) sum += exchange[(p * most + unit - u0) * 32 + lane];
-                finish(a, column, row0 + (unit >> 2), sum);
+            const int c1 = min(valid, static_cast<int>(rank + 1) * each);
+            for (int c0 = rank * each; c0 < c1; c0 += 8) {
+                float z[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) z[i] = 0.0f;
+                for (uint32_t p = 0; p < splits; ++p) {
+                    const float* from = exchange + (p * each + c0 - rank * each) * kTileM + quarter * 32 + lane;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) z[i] += c0 + i < c1 ? from[i * kTileM] : 0.0f;
+                }
+                finish<T, 8>(a, column, row0 + c0, c1 - c0, z);
             }
         }
     }
@@ -289,6 +319,181 @@ int codes_map(const void* base, int planes, int rows, int k, int box_planes, int
     return encode_map(CU_TENSOR_MAP_DATA_TYPE_UINT8, box_planes ? 3 : 2, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, out);
 }
 
+// ---- many rows ----
+// A pair of CTAs on neighbouring SMs (cta_group::2, M = 256) has 256 rows of W by up to 256 of x: each CTA fetches 128 rows of W and
+// half of the rows of x, so a byte of either is used twice as often as by a CTA alone.  Persistent, one CTA per SM: a warp feeds
+// the ring, a warp of the even CTA issues the MMAs, eight warps drain the accumulators, of which there are two: the next tile is
+// multiplied while the last is finished and written.
+constexpr int kEpilogueWarps = 8;
+constexpr int kWideThreads = 32 * (2 + kEpilogueWarps);
+
+__device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+// Boxes into this CTA's shared memory, their bytes counted on `bar` (an address in either CTA of the pair).
+__device__ __forceinline__ void tma_pair_2d(void* dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+        ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void tma_pair_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void mma_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t"
+        "}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// One arrival on the barrier at this offset in both CTAs once every MMA issued so far has finished.
+__device__ __forceinline__ void commit_pair(uint64_t* bar) {
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+        ::"r"(smem_u32(bar)), "h"(static_cast<uint16_t>(3))
+        : "memory");
+}
+__device__ __forceinline__ void arrive_at(uint32_t cluster_addr) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+
+// grid = 2 * pairs, clusters of 2, block = kWideThreads.
+template <typename T>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWideThreads, 1)
+linear_fp8_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ LinearArgs a) {
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    const int half = a.tokens / 2, stage_bytes = kTileBytes + half * kBlockK;
+    uint64_t* full_bar = reinterpret_cast<uint64_t*>(smem + a.stages * stage_bytes);  // (the even CTA's count both CTAs' bytes)
+    uint64_t* empty_bar = full_bar + kMaxStages;
+    uint64_t* acc_full = empty_bar + kMaxStages;  // [2]
+    uint64_t* acc_empty = acc_full + 2;           // [2], the even CTA's count both CTAs' epilogue warps
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+
+    const int warp = __shfl_sync(kFullMask, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < a.stages; ++s) {
+            mbar_init(&full_bar[s], 1);
+            mbar_init(&empty_bar[s], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&acc_full[i], 1);
+            mbar_init(&acc_empty[i], 2 * kEpilogueWarps);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster_sync_all();  // both CTAs' barriers exist
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = *tmem_slot;
+    bool ok = true;
+    pdl_wait();
+    pdl_trigger();
+
+    if (warp == 0) {
+        const bool leader = elect_one(), gated = a.act >= kActGatedGelu;
+        const uint32_t full0 = in_cta(smem_u32(full_bar), 0);
+        int s = 0, use = 0;
+        for (int tile = pair; ok && tile < a.tiles; tile += pairs) {
+            const int w_tile = (tile / a.token_tiles) * 2 + static_cast<int>(rank);  // of 128 rows
+            const int row0 = (tile % a.token_tiles) * a.tokens + static_cast<int>(rank) * half;
+            for (int kb = 0; kb < a.k_blocks; ++kb) {
+                if (use > 0 && !mbar_wait_warp(&empty_bar[s], (use - 1) & 1, a.limit)) { ok = false; break; }
+                if (leader) {
+                    uint8_t* stage = smem + s * stage_bytes;
+                    if (rank == 0) mbar_expect_tx(&full_bar[s], 2 * stage_bytes);
+                    if (gated) {
+                        for (int i = 0; i < 4; ++i) tma_pair_3d(stage + i * (kTileBytes / 4), &map_w, kb * kBlockK, w_tile * (kTileM / 2) + 16 * i, 0, full0 + 8 * s);
+                    } else {
+                        tma_pair_3d(stage, &map_w, kb * kBlockK, w_tile * kTileM, 0, full0 + 8 * s);
+                    }
+                    tma_pair_2d(stage + kTileBytes, &map_x, kb * kBlockK, row0, full0 + 8 * s);
+                }
+                if (++s == a.stages) { s = 0; ++use; }
+            }
+        }
+        if (!ok && rank == 0)  // nothing may still be on its way when the CTAs leave
+            for (int i = 0; i < a.stages; ++i) {
+                mbar_wait(&full_bar[i], 0, kDrainLimit);
+                mbar_wait(&full_bar[i], 1, kDrainLimit);
+            }
+    } else if (warp == 1) {
+        if (rank == 0) {
+            const bool leader = elect_one();
+            const uint32_t idesc = instr_desc_e4m3(2 * kTileM, a.tokens);
+            const uint32_t base = smem_u32(smem);
+            int s = 0, use = 0;     // stage, and how often the ring has gone round
+            int buf = 0, turn = 0;  // accumulator, and how often both have had their turn
+            for (int tile = pair; ok && tile < a.tiles; tile += pairs) {
+                if (turn > 0 && !mbar_wait_warp(&acc_empty[buf], (turn - 1) & 1, a.limit)) { ok = false; break; }
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                for (int kb = 0; kb < a.k_blocks; ++kb) {
+                    if (!mbar_wait_warp(&full_bar[s], use & 1, a.limit)) { ok = false; break; }
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint64_t w_desc = smem_desc_sw128(base + s * stage_bytes), x_desc = smem_desc_sw128(base + s * stage_bytes + kTileBytes);
+                    if (leader) {
+#pragma unroll
+                        for (int k = 0; k < kBlockK / kCodesK; ++k)
+                            mma_pair(tmem + buf * 256, w_desc + ((k * kCodesK) >> 4), x_desc + ((k * kCodesK) >> 4), idesc, kb > 0 || k > 0 ? 1u : 0u);
+                        commit_pair(&empty_bar[s]);
+                    }
+                    __syncwarp();
+                    if (++s == a.stages) { s = 0; ++use; }
+                }
+                if (ok && leader) commit_pair(&acc_full[buf]);
+                __syncwarp();
+                if (++buf == 2) { buf = 0; ++turn; }
+            }
+        }
+    } else {
+        const int quarter = warp & 3, first_col = ((warp - 2) >> 2) * 16;
+        int buf = 0, turn = 0;
+        for (int tile = pair; tile < a.tiles; tile += pairs) {
+            const LaneColumn column = lane_column(a, (tile / a.token_tiles) * 2 + static_cast<int>(rank), quarter, lane);
+            const int row0 = (tile % a.token_tiles) * a.tokens, valid = min(a.tokens, a.rows - row0);
+            if (!mbar_wait_warp(&acc_full[buf], turn & 1, a.limit)) { ok = false; break; }
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t acc = tmem + buf * 256 + (static_cast<uint32_t>(quarter * 32) << 16);
+            for (int c0 = first_col; c0 < valid; c0 += 32) {
+                float z[16];
+                tmem_ld16(acc + c0, reinterpret_cast<uint32_t(&)[16]>(z));
+                tmem_ld_wait();
+                finish<T, 16>(a, column, row0 + c0, valid - c0, z);
+            }
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) arrive_at(in_cta(smem_u32(&acc_empty[buf]), 0));
+            if (++buf == 2) { buf = 0; ++turn; }
+        }
+    }
+    if (!ok) atomicCAS(&g_linear_error, 0, 16 + warp);
+    __syncwarp();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    cluster_sync_all();  // nobody leaves while its peer may still signal or read its shared memory
+    if (warp == 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
+    }
+}
+
+template <typename T>
 int launch_small(const void* x, const void* w, int k, LinearArgs a, cudaStream_t stream) {
     const bool gated = a.act >= kActGatedGelu;
     const int per_tile = gated ? kTileM / 2 : kTileM, tiles = (a.n_out + per_tile - 1) / per_tile;
@@ -297,20 +502,54 @@ int launch_small(const void* x, const void* w, int k, LinearArgs a, cudaStream_t
     a.tokens = ((a.rows + token_tiles - 1) / token_tiles + 15) / 16 * 16;
     token_tiles = (a.rows + a.tokens - 1) / a.tokens;
     int splits = 1;
+    static const int fs = getenv("LIN_S") ? atoi(getenv("LIN_S")) : 0, fst = getenv("LIN_ST") ? atoi(getenv("LIN_ST")) : 99;
+    if (fs) splits = std::min(fs, a.k_blocks); else
     while (splits < 8 && tiles * token_tiles * splits * 2 <= 148 && splits * 2 <= a.k_blocks) splits *= 2;
-    const int stage_bytes = kTileBytes + a.tokens * kBlockK, exchange = splits > 1 ? a.tokens * kTileM * 4 : 0;
+    const int stage_bytes = kTileBytes + a.tokens * kBlockK, exchange = exchange_bytes(a.tokens, splits);
     a.stages = std::min({kMaxStages, (227 * 1024 - 1024 - 512 - exchange) / stage_bytes, std::max(2, (a.k_blocks + splits - 1) / splits)});
+    a.stages = std::min(a.stages, fst);
     CUtensorMap mw, mx;
     int status = codes_map(w, gated ? 2 : 1, a.n_out, k, gated ? 2 : 1, gated ? 16 : kTileM, &mw);
     if (status == SPEC_OK) status = codes_map(x, 1, a.rows, k, 0, a.tokens, &mx);
     if (status != SPEC_OK) return status;
     static std::atomic<unsigned long long> configured{0};
-    status = allow_shared_memory(configured, linear_fp8_kernel, 227 * 1024);
+    status = allow_shared_memory(configured, linear_fp8_kernel<T>, 227 * 1024);
     if (status != SPEC_OK) return status;
     // 48 KB and more: at most four CTAs to an SM, whose tensor memory (128 columns each) then all fits.  A CTA that had to wait for
     // columns while its cluster waits for it could wait for ever.
     const int smem = std::max(48 * 1024, a.stages * stage_bytes + exchange + 1024 + 512);
-    return launch_cluster(linear_fp8_kernel, splits, dim3(tiles * splits, token_tiles), dim3(kThreads), smem, stream, mw, mx, a);
+    return launch_cluster(linear_fp8_kernel<T>, splits, dim3(tiles * splits, token_tiles), dim3(kThreads), smem, stream, mw, mx, a);
+}
+
+template <typename T>
+int launch_wide(const void* x, const void* w, int k, LinearArgs a, cudaStream_t stream) {
+    const bool gated = a.act >= kActGatedGelu;
+    constexpr int kPairs = 74;  // one CTA per SM
+    const int per_tile = gated ? kTileM : 2 * kTileM, w_tiles = (a.n_out + per_tile - 1) / per_tile;
+    a.k_blocks = (k + kBlockK - 1) / kBlockK;
+    // Rows of x per tile: as many as make the busiest pair's tiles the shortest (a tile costs its columns and about as much again as
+    // 16 for its start).
+    long long best = 0;
+    for (int tokens = 256; tokens >= 64; tokens -= 16) {
+        const int token_tiles = (a.rows + tokens - 1) / tokens;
+        const long long rounds = (static_cast<long long>(w_tiles) * token_tiles + kPairs - 1) / kPairs, cost = rounds * (tokens + 16);
+        if (best == 0 || cost < best) {
+            best = cost;
+            a.tokens = tokens;
+            a.token_tiles = token_tiles;
+        }
+    }
+    a.tiles = w_tiles * a.token_tiles;
+    const int stage_bytes = kTileBytes + a.tokens / 2 * kBlockK;
+    a.stages = std::min(kMaxStages, (227 * 1024 - 1024 - 512) / stage_bytes);
+    CUtensorMap mw, mx;
+    int status = codes_map(w, gated ? 2 : 1, a.n_out, k, gated ? 2 : 1, gated ? 16 : kTileM, &mw);
+    if (status == SPEC_OK) status = codes_map(x, 1, a.rows, k, 0, a.tokens / 2, &mx);
+    if (status != SPEC_OK) return status;
+    static std::atomic<unsigned long long> configured{0};
+    status = allow_shared_memory(configured, linear_fp8_wide_kernel<T>, 227 * 1024);
+    if (status != SPEC_OK) return status;
+    return launch_pdl(linear_fp8_wide_kernel<T>, dim3(2 * std::min(kPairs, a.tiles)), dim3(kWideThreads), a.stages * stage_bytes + 1024 + 512, stream, mw, mx, a);
 }
 
 }  // namespace
@@ -344,7 +583,11 @@ extern "C" int spec_linear_fp8(const void* x, const float* x_scales, const void*
     a.rows = rows;
     a.n_out = n_out;
     a.act = act;
-    a.y_dtype = y_dtype;
     a.limit = tc::kSpinLimit;
-    return launch_small(x, w, k, a, static_cast<cudaStream_t>(stream));
+    static const int wide_from = getenv("LIN_WIDE") ? atoi(getenv("LIN_WIDE")) : 129;
+    const auto go = [&](auto type) {
+        using T = decltype(type);
+        return rows >= wide_from ? launch_wide<T>(x, w, k, a, static_cast<cudaStream_t>(stream)) : launch_small<T>(x, w, k, a, static_cast<cudaStream_t>(stream));
+    };
+    return y_dtype == SPEC_DTYPE_FP32 ? go(float{}) : y_dtype == SPEC_DTYPE_BF16 ? go(__nv_bfloat16{}) : go(__half{});
 }
