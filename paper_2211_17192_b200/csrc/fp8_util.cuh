@@ -36,26 +36,9 @@ __device__ __forceinline__ uint32_t codes_int8(float x, float y) {
     return (a & 0xff) | ((b & 0xff) << 8);
 }
 
-// Four elements from memory as fp32, and back; `wide`: the address is aligned to all four.
-__device__ __forceinline__ void load4(const float* p, bool wide, float (&v)[4]) {
-    if (wide) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(p);
-    else
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = p[i];
-}
 __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
 __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float to_float(float v) { return v; }
-template <typename T>
-__device__ __forceinline__ void load4(const T* p, bool wide, float (&v)[4]) {
-    T t[4];
-    if (wide) *reinterpret_cast<uint2*>(t) = *reinterpret_cast<const uint2*>(p);
-    else
-#pragma unroll
-        for (int i = 0; i < 4; ++i) t[i] = p[i];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = to_float(t[i]);
-}
 template <typename T>
 __device__ __forceinline__ T from_float(float v);
 template <>
@@ -64,17 +47,38 @@ template <>
 __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
-template <typename T>
-__device__ __forceinline__ void store4(T* p, bool wide, const float (&v)[4]) {
-    T t[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) t[i] = from_float<T>(v[i]);
+
+// N elements from memory as fp32, and back; `wide`: the address is aligned to 16 bytes, or to all of them where they are fewer.
+template <int N, typename T>
+__device__ __forceinline__ void load_row(const T* p, bool wide, float (&v)[N]) {
+    constexpr int kBytes = N * sizeof(T);
+    __align__(16) T t[N];
     if (wide) {
-        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(p) = *reinterpret_cast<const float4*>(t);
-        else *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(t);
+        if constexpr (kBytes == 8) *reinterpret_cast<uint2*>(t) = *reinterpret_cast<const uint2*>(p);
+        else
+#pragma unroll
+            for (int i = 0; i < kBytes / 16; ++i) reinterpret_cast<uint4*>(t)[i] = reinterpret_cast<const uint4*>(p)[i];
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = t[i];
+        for (int i = 0; i < N; ++i) t[i] = p[i];
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = to_float(t[i]);
+}
+template <int N, typename T>
+__device__ __forceinline__ void store_row(T* p, bool wide, const float (&v)[N]) {
+    constexpr int kBytes = N * sizeof(T);
+    __align__(16) T t[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) t[i] = from_float<T>(v[i]);
+    if (wide) {
+        if constexpr (kBytes == 8) *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(t);
+        else
+#pragma unroll
+            for (int i = 0; i < kBytes / 16; ++i) reinterpret_cast<uint4*>(p)[i] = reinterpret_cast<const uint4*>(t)[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) p[i] = t[i];
     }
 }
 

@@ -14,7 +14,6 @@
 // Every wait on an mbarrier is bounded; on expiry the kernel records an error code, waits (with a limit) for its copies and
 // leaves, tensor memory freed.
 #include <algorithm>
-#include <cstdlib>
 
 #include "fp8_util.cuh"
 #include "tc_util.cuh"
@@ -87,14 +86,15 @@ __device__ __forceinline__ void cluster_sync_all() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ void store_peer(uint32_t here, uint32_t rank, float v) {
+__device__ __forceinline__ void store_peer(uint32_t here, uint32_t rank, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
     uint32_t there;
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(here), "r"(rank));
-    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there), "f"(v) : "memory");
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(there), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
 
-// The columns that a CTA of a cluster finishes, from each of its CTAs.
-__host__ __device__ __forceinline__ int exchange_bytes(int tokens, int splits) { return splits > 1 ? splits * ((tokens + splits - 1) / splits) * kTileM * 4 : 0; }
+// The columns that a CTA of a cluster finishes (in fours, as they are exchanged), and the place of these from each of its CTAs.
+__host__ __device__ __forceinline__ int columns_each(int columns, int splits) { return ((columns + 3) / 4 + splits - 1) / splits * 4; }
+__host__ __device__ __forceinline__ int exchange_bytes(int tokens, int splits) { return splits > 1 ? splits * columns_each(tokens, splits) * kTileM * 4 : 0; }
 
 // What a lane of an epilogue warp knows of its accumulator lane (row of W), constant over a tile.
 struct LaneColumn {
@@ -265,8 +265,8 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
                 finish<T, 16>(a, column, row0 + c0, valid - c0, z);
             }
     } else {
-        // CTA r finishes columns [r each, (r + 1) each): the others' sums of these lie in its exchange as [CTA][column][128]
-        const int each = (valid + splits - 1) / splits;
+        // CTA r finishes columns [r each, (r + 1) each): the others' sums of these lie in its exchange as [CTA][four columns][128][4]
+        const int each = columns_each(valid, splits);
         asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // everyone is there
         if (reader && ok)
             for (int c0 = 0; c0 < valid; c0 += 16) {
@@ -279,10 +279,10 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
                 }
                 int to = c0 / each, within = c0 - to * each;
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
+                for (int i = 0; i < 16; i += 4)
                     if (c0 + i < valid) {
-                        store_peer(smem_u32(exchange + (rank * each + within) * kTileM + quarter * 32 + lane), to, __uint_as_float(v[i]));
-                        if (++within == each) { within = 0; ++to; }
+                        store_peer(smem_u32(exchange + (rank * each + within) * kTileM + (quarter * 32 + lane) * 4), to, v[i], v[i + 1], v[i + 2], v[i + 3]);
+                        if ((within += 4) == each) { within = 0; ++to; }
                     }
             }
         cluster_sync_all();
@@ -293,9 +293,16 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
 #pragma unroll
                 for (int i = 0; i < 8; ++i) z[i] = 0.0f;
                 for (uint32_t p = 0; p < splits; ++p) {
-                    const float* from = exchange + (p * each + c0 - rank * each) * kTileM + quarter * 32 + lane;
+                    const float4* from = reinterpret_cast<const float4*>(exchange + (p * each + c0 - rank * each) * kTileM) + quarter * 32 + lane;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) z[i] += c0 + i < c1 ? from[i * kTileM] : 0.0f;
+                    for (int i = 0; i < 8; i += 4) {
+                        if (c0 + i >= c1) continue;
+                        const float4 v = from[i / 4 * kTileM];
+                        z[i] += v.x;
+                        z[i + 1] += v.y;
+                        z[i + 2] += v.z;
+                        z[i + 3] += v.w;
+                    }
                 }
                 finish<T, 8>(a, column, row0 + c0, c1 - c0, z);
             }
@@ -501,13 +508,17 @@ int launch_small(const void* x, const void* w, int k, LinearArgs a, cudaStream_t
     int token_tiles = (a.rows + 127) / 128;
     a.tokens = ((a.rows + token_tiles - 1) / token_tiles + 15) / 16 * 16;
     token_tiles = (a.rows + a.tokens - 1) / a.tokens;
+    // One wave, all CTAs resident (a second wave starts behind the first one's epilogue: 4096 x 6144, three rows, three CTAs to a
+    // cluster and one to an SM 11.8 us, since such clusters do not fill the SMs; four, two to an SM 7.6).  Up to 64 columns two
+    // CTAs share an SM, and clusters grow while there are at most 200 CTAs; above, the exchange takes too much room, and clusters
+    // of at most four can be placed as long as there are 128 CTAs (of eight, some wait: 112 x 2000 x 2000 14.6 us, 9 with four).
+    const bool paired = a.tokens <= 64;
     int splits = 1;
-    static const int fs = getenv("LIN_S") ? atoi(getenv("LIN_S")) : 0, fst = getenv("LIN_ST") ? atoi(getenv("LIN_ST")) : 99;
-    if (fs) splits = std::min(fs, a.k_blocks); else
-    while (splits < 8 && tiles * token_tiles * splits * 2 <= 148 && splits * 2 <= a.k_blocks) splits *= 2;
+    for (int s = 2; s <= (paired ? 8 : 4); ++s)
+        if (tiles * token_tiles * s <= (paired ? 200 : 128) && 2 * s <= a.k_blocks) splits = s;
     const int stage_bytes = kTileBytes + a.tokens * kBlockK, exchange = exchange_bytes(a.tokens, splits);
-    a.stages = std::min({kMaxStages, (227 * 1024 - 1024 - 512 - exchange) / stage_bytes, std::max(2, (a.k_blocks + splits - 1) / splits)});
-    a.stages = std::min(a.stages, fst);
+    const int room = (paired ? 113 : 227) * 1024 - 1024 - 512 - exchange;
+    a.stages = std::min({kMaxStages, room / stage_bytes, std::max(2, (a.k_blocks + splits - 1) / splits)});
     CUtensorMap mw, mx;
     int status = codes_map(w, gated ? 2 : 1, a.n_out, k, gated ? 2 : 1, gated ? 16 : kTileM, &mw);
     if (status == SPEC_OK) status = codes_map(x, 1, a.rows, k, 0, a.tokens, &mx);
@@ -584,10 +595,14 @@ extern "C" int spec_linear_fp8(const void* x, const float* x_scales, const void*
     a.n_out = n_out;
     a.act = act;
     a.limit = tc::kSpinLimit;
-    static const int wide_from = getenv("LIN_WIDE") ? atoi(getenv("LIN_WIDE")) : 129;
+    // CTA pairs fetch half as much per product, clusters that share a tile's k-blocks use more SMs where tiles are few.  11008 x 4096:
+    // 192 rows 18.0 us in clusters and 20.2 in pairs, 256 rows 20.2 and 20.1; 4096 x 4096: 96 rows 9.3 and 10.4, 192 rows 11.9 and
+    // 10.8; 768 x 2304: 80 rows 6.1 and 4.9; 4096 x 6144 (48 tiles): 64 rows 10.2 and 10.6, 80 rows 11.3 and 10.7.
+    const int tiles = (n_out + (act >= kActGatedGelu ? 63 : 127)) / (act >= kActGatedGelu ? 64 : 128), k_blocks = (k + kBlockK - 1) / kBlockK;
+    const bool wide = rows > 64 && (tiles > 37 || rows > 64 + k_blocks + k_blocks / 2);
     const auto go = [&](auto type) {
         using T = decltype(type);
-        return rows >= wide_from ? launch_wide<T>(x, w, k, a, static_cast<cudaStream_t>(stream)) : launch_small<T>(x, w, k, a, static_cast<cudaStream_t>(stream));
+        return wide ? launch_wide<T>(x, w, k, a, static_cast<cudaStream_t>(stream)) : launch_small<T>(x, w, k, a, static_cast<cudaStream_t>(stream));
     };
     return y_dtype == SPEC_DTYPE_FP32 ? go(float{}) : y_dtype == SPEC_DTYPE_BF16 ? go(__nv_bfloat16{}) : go(__half{});
 }

@@ -387,8 +387,8 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
             if (there && lane < D / 4) {
                 const int head = g.head * a.group + query - i * a.group;
                 const size_t at = (static_cast<size_t>(b) * a.rows + i) * a.q_stride + head * D + 4 * lane;
-                if (a.q_bf16) load4(static_cast<const __nv_bfloat16*>(a.q) + at, true, v);
-                else load4(static_cast<const __half*>(a.q) + at, true, v);
+                if (a.q_bf16) load_row(static_cast<const __nv_bfloat16*>(a.q) + at, true, v);
+                else load_row(static_cast<const __half*>(a.q) + at, true, v);
             }
             float back = 1.0f;
             if constexpr (!S::kBf16) {
@@ -645,8 +645,8 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                         const float v[4] = {o[n][2 * h] * by, o[n + 1][2 * h] * by, o[n][2 * h + 1] * by, o[n + 1][2 * h + 1] * by};
                         const int dim = 8 * n + 4 * c;
                         if (!whole) *reinterpret_cast<float4*>(part + dim) = *reinterpret_cast<const float4*>(v);
-                        else if (a.q_bf16) store4(static_cast<__nv_bfloat16*>(a.out) + at + dim, true, v);
-                        else store4(static_cast<__half*>(a.out) + at + dim, true, v);
+                        else if (a.q_bf16) store_row(static_cast<__nv_bfloat16*>(a.out) + at + dim, true, v);
+                        else store_row(static_cast<__half*>(a.out) + at + dim, true, v);
                     } else {
 #pragma unroll
                         for (int m = 0; m < 2; ++m) {

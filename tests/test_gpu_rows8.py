@@ -14,7 +14,7 @@ def normal(seed, *shape):
     return torch.from_numpy(np.random.default_rng(seed).standard_normal(shape, dtype=np.float32))
 
 
-@pytest.mark.parametrize("rows,d", [(1, 1), (1, 768), (3, 7), (5, 252), (2, 33), (300, 128), (7, 4096), (2, 4104), (3, 11008), (2, 11003), (2, 16384), (1, 32768)])
+@pytest.mark.parametrize("rows,d", [(1, 1), (1, 768), (3, 7), (5, 252), (2, 33), (300, 128), (7, 4096), (2, 4104), (3, 11008), (2, 11003), (2, 16384), (1, 32768), (900, 4096), (500, 1544), (1000, 11008), (450, 16384)])
 @pytest.mark.parametrize("dtype", [F32, BF16, F16])
 def test_quantize(rows, d, dtype):
     x = (normal(rows * 100003 + d, rows, d) * 3).to(dtype)
@@ -48,7 +48,7 @@ def test_quantize_unaligned_and_extreme_rows():
 NORM_REL = (42 / 2 + 6) * 2.0 ** -24
 
 
-@pytest.mark.parametrize("rows,d", [(1, 1), (1, 768), (4, 7), (2, 250), (130, 256), (3, 4096), (2, 8200), (2, 11008), (1, 32768)])
+@pytest.mark.parametrize("rows,d", [(1, 1), (1, 768), (4, 7), (2, 250), (130, 256), (3, 4096), (2, 8200), (2, 11008), (1, 32768), (900, 4096), (500, 1544), (450, 11008)])
 @pytest.mark.parametrize("dtype,h_dtype", [(F32, F32), (BF16, F32), (BF16, BF16), (F16, F32), (F16, F16)])
 def test_norm(rows, d, dtype, h_dtype):
     x, gain = (normal(d, rows, d) * 2).to(dtype), 1 + 0.1 * normal(d + 1, d)
