@@ -9,13 +9,17 @@
 // about 1 whatever the scales are, and one exponential per score serves both sums.
 //
 // Work: tiles of 64 keys of a segment (sequence, block of queries, KV head).  The lengths are known on the device only, so every
-// CTA adds them up and takes an equal, contiguous run of all tiles (the longest sequence does not decide, whatever the capacity of
-// the page table); a segment that several CTAs share leaves (maximum, sum, weighted rows) per CTA in the workspace, and a second
+// CTA adds them up and takes an equal, contiguous run of all slots (the longest sequence does not decide, whatever the capacity of
+// the page table): a segment has a slot per tile and kSwitch more in front of them, since the CTAs with many short segments decide
+// else.  A segment that several CTAs share leaves (maximum, sum, weighted rows) per CTA in the workspace, and a second
 // kernel joins them in order.  No atomics: the same bits every time.
 //
-// A CTA has four groups of warps; a group takes 16 of a tile's 64 keys, a warp of it 16 queries.  One more warp asks for the tiles
-// of the whole run, segment after segment, by TMA (halves of 32 keys, which never straddle a page, with the shared-memory
-// swizzle), through a ring of stages with a barrier to fill and one to free each; the others never wait for one another within a segment.
+// A CTA has four warps, each with 16 of a tile's 64 keys and all queries of the block, 8, 16 or 32.  The keys take the M side of both
+// products (scores [key][query], weighted rows [dim][query]): queries come in eights then, and a K or V fragment is widened once
+// for all of them.  (Queries on the M side, sixteen at least: twice the multiplications and registers for a lone token of four
+// heads.)  One more warp asks for the tiles of the whole run, segment after segment, by TMA (halves of 32 keys, which never straddle a
+// page, with the shared-memory swizzle) through a ring of stages with a barrier to fill and one to free each; a warp's queries
+// are on their way a segment ahead.  The four never wait for one another within a segment.
 #include <algorithm>
 
 #include "paged.cuh"
@@ -27,9 +31,10 @@ namespace {
 using namespace tc;
 
 constexpr int kTileKeys = 64;
-constexpr int kGroups = 4;       // warps along a tile's keys, 16 keys each
-constexpr int kMostCtas = 592;   // 148 SMs x 4
+constexpr int kWarps = 4;        // that compute, with 16 of a tile's keys each
+constexpr int kMostCtas = 148 * 4;
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kSwitch = 3;       // tiles that taking up another segment costs about as much as
 constexpr float kSlack = 8.0f;   // the running maximum may lag by this: w <= 2^8 stays in fp16's range
 
 __device__ int g_paged_error;  // set when the bounded wait for a tile or for its place ran out (0 = none)
@@ -47,6 +52,9 @@ struct AttnArgs {
     float scale;
     int batch, rows, n_heads, group, blocks, units;  // blocks: of queries per (sequence, KV head); units = batch * blocks
     int q_bf16, grid;
+    uint32_t by_group;  // ceil(2^32 / group) for groups of two and more
+    // The token of a query of a (sequence, KV head); exact, since query * group stays below 2^31.
+    __device__ __forceinline__ int token_of(int query) const { return group == 1 ? query : static_cast<int>(__umulhi(static_cast<uint32_t>(query), by_group)); }
 };
 
 // Copies that count their bytes on a barrier: a box of 32 rows of a plane (K or V of a page and head), and a run of bytes.
@@ -60,6 +68,9 @@ __device__ __forceinline__ void load_bulk(void* to, const void* from, int bytes,
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(smem_u32(to)), "l"(from), "r"(bytes), "r"(smem_u32(bar)) : "memory");
 }
+__device__ __forceinline__ void copy8(void* to, const void* from, bool there) {  // (zeros where there is nothing)
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(there ? 8 : 0) : "memory");
+}
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
@@ -72,6 +83,11 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint4& a, uint32_t
     else
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t v) {  // an 8 x 8 tile of 16-bit values across the warp
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
 }
 __device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
@@ -138,77 +154,86 @@ __device__ __forceinline__ bool not_numbers(const uint4& v) {
     return any;
 }
 
-// One segment of a CTA's run of tiles.
-struct Segment {
-    int unit, head, tile0, tile1, tiles, limit;  // limit: keys before it exist for some row of the block
-};
-
-// Tiles of a unit (sequence, block of queries): the keys up to the position of the block's last row.
+// Keys of a unit (sequence, block of queries): those up to the position of the block's last row.
 template <int QT>
 __device__ __forceinline__ int unit_limit(const AttnArgs& a, int unit) {
-    const int b = unit / a.blocks, block = unit - b * a.blocks;
-    const long long capacity = static_cast<long long>(a.cache.width) << a.cache.page_shift;
+    const int b = a.blocks == 1 ? unit : unit / a.blocks, block = unit - b * a.blocks;
+    const int capacity = a.cache.width << a.cache.page_shift;
     const int length = a.lengths[b];
-    const int last_row = min(a.rows - 1, (block * QT + QT - 1) / a.group);
-    const long long limit = static_cast<long long>(length) - a.rows + last_row + 1;
-    return static_cast<int>(max(0ll, min(min(limit, static_cast<long long>(length)), capacity)));
+    const int last_row = min(a.rows - 1, a.token_of(block * QT + QT - 1));
+    return min(max(0, max(length, 0) - (a.rows - 1 - last_row)), capacity);
 }
+// Slots of a (unit, KV head): its tiles, and kSwitch more for taking it up, if there are any.
+__device__ __forceinline__ int unit_slots(int limit) { return limit > 0 ? (limit + kTileKeys - 1) / kTileKeys + kSwitch : 0; }
 
-// The unit in which tile `wanted` of all lies, with the tiles (of one KV head) before it; and the sum over all units.
-// `wanted(total)` is called once the sum is known.  All threads of the block; `scratch`: 40 long longs.
-template <int QT, typename F>
-__device__ __forceinline__ void find_unit(const AttnArgs& a, long long* scratch, F wanted, long long& total, int& unit, long long& before) {
+// How all slots are shared out: CTA c has the run [first(c), first(c + 1)).
+struct Shares {
+    int total, ctas, each, more;  // `more` CTAs have one slot above `each`
+    __device__ __forceinline__ Shares(int sum, int grid) : total(sum), ctas(max(1, min(sum, grid))) {
+        each = static_cast<int>(static_cast<uint32_t>(sum) / static_cast<uint32_t>(ctas));
+        more = sum - each * ctas;
+    }
+    __device__ __forceinline__ int first(int cta) const { return cta * each + min(cta, more); }
+    __device__ __forceinline__ int owner(int slot) const {
+        const int large = more * (each + 1);
+        return slot < large ? static_cast<int>(static_cast<uint32_t>(slot) / static_cast<uint32_t>(each + 1))
+                            : more + static_cast<int>(static_cast<uint32_t>(slot - large) / static_cast<uint32_t>(each));
+    }
+};
+
+// The sum of all units' slots (times the KV heads), and the unit in which this CTA's run begins (-1: it has none) with the slots of one
+// KV head before it.  All threads of the block; `scratch`: 24 ints.
+template <int QT>
+__device__ __forceinline__ int find_unit(const AttnArgs& a, int* scratch, int& unit, int& before) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-    long long base = 0, target = 0;
+    const bool fits = a.units <= static_cast<int>(blockDim.x);  // (else: add up first, look then)
+    int total = 0, target = 0, base = 0;
     unit = -1;
-    for (int round = a.units > static_cast<int>(blockDim.x) ? 0 : 1; round < 2; ++round) {  // (more units than threads: add up first, look then)
-        if (round == 1 && a.units > static_cast<int>(blockDim.x)) {
+    for (int round = fits ? 1 : 0; round < 2; ++round) {
+        if (round == 1 && !fits) {
             total = base * a.cache.n_kv;
-            target = wanted(total);
+            target = Shares(total, a.grid).first(blockIdx.x);
             base = 0;
         }
         for (int u0 = 0; u0 < a.units; u0 += blockDim.x) {
             const int u = u0 + threadIdx.x;
-            const long long mine = u < a.units ? (unit_limit<QT>(a, u) + kTileKeys - 1) / kTileKeys : 0;
-            long long upto = mine;
+            const int mine = u < a.units ? unit_slots(unit_limit<QT>(a, u)) : 0;
+            int upto = mine;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
-                const long long up = __shfl_up_sync(kFullMask, upto, o);
+                const int up = __shfl_up_sync(kFullMask, upto, o);
                 if (lane >= o) upto += up;
             }
             __syncthreads();  // (scratch is free)
             if (lane == 31) scratch[warp] = upto;
             __syncthreads();
-            long long all = 0, front = 0;
+            int all = 0, front = 0;
             for (int w = 0; w < warps; ++w) {
                 if (w < warp) front += scratch[w];
                 all += scratch[w];
             }
             upto += base + front;
             if (round == 1) {
-                if (a.units <= static_cast<int>(blockDim.x)) {
+                if (fits) {
                     total = all * a.cache.n_kv;
-                    target = wanted(total);
+                    target = Shares(total, a.grid).first(blockIdx.x);
                 }
                 if ((upto - mine) * a.cache.n_kv <= target && target < upto * a.cache.n_kv) {
-                    scratch[32] = u;
-                    scratch[33] = upto - mine;
+                    scratch[16] = u;
+                    scratch[17] = upto - mine;
                 }
             }
             base += all;
         }
     }
-    if (total == 0 || target >= total) return;
+    if (static_cast<int>(blockIdx.x) >= Shares(total, a.grid).ctas || total == 0) return total;
     __syncthreads();
-    unit = static_cast<int>(scratch[32]);
-    before = scratch[33];
+    unit = scratch[16];
+    before = scratch[17];
+    return total;
 }
 
-__device__ __forceinline__ long long first_tile(long long total, int cta, int ctas) { return total * cta / ctas; }
-__device__ __forceinline__ int owner_of(long long total, long long tile, int ctas) { return static_cast<int>(((tile + 1) * ctas - 1) / total); }
-__device__ __forceinline__ int ctas_of(long long total, int grid) { return static_cast<int>(min(total, static_cast<long long>(grid))); }
-
-template <int D, int KV, int MT>
+template <int D, int KV, int NT>
 struct Shape {
     static constexpr bool kEight = KV == SPEC_DTYPE_E4M3 || KV == SPEC_DTYPE_INT8;
     static constexpr bool kBf16 = KV == SPEC_DTYPE_BF16;
@@ -216,16 +241,20 @@ struct Shape {
     static constexpr int kBoxBytes = kRowBytes < 128 ? kRowBytes : 128;  // of a row in one copy: what the swizzle spans
     static constexpr int kBoxes = kRowBytes / kBoxBytes;
     static constexpr int kChunks = kRowBytes / 16;
-    static constexpr int kQueries = 16 * MT;
-    static constexpr int kComputeWarps = kGroups * MT;
-    static constexpr int kThreads = 32 * (kComputeWarps + 1);  // and the warp that asks for the tiles
+    static constexpr int kQueries = 8 * NT;
+    // The warp that fetches is one more; 32 queries of 128 dims need more registers than two CTAs of five warps leave to a thread
+    // (168), so there it is one of four, whose registers the others take over.
+    static constexpr bool kShift = D == 128 && NT == 4;
+    static constexpr int kThreads = 32 * (kShift ? 2 * kWarps : kWarps + 1);
+    static constexpr int kTaken = 224, kLeft = 32;  // registers then: their sum is twice the 128 of the launch
     static constexpr int kOperandBytes = kTileKeys * kRowBytes;  // K or V of a tile
     static constexpr int kStageBytes = 2 * kOperandBytes;
     static constexpr int kScaleBytes = kEight ? 2 * kTileKeys * 4 : 0;
     static constexpr int kQueryBytes = kQueries * D * 2;
-    static constexpr int kMerge = 2 * MT * 16 * (D + 2) * 4;  // two groups' states
-    static constexpr int kPerSm = MT == 1 ? (kRowBytes <= 128 ? 3 : 2) : 1;
-    static constexpr int kFixed = kMerge + kQueryBytes + kQueries * 4 + 40 * 8 + 1024 /* alignment */ + 256 /* barriers, notes */;
+    static constexpr int kJoined = NT < 2 ? NT : 2;             // eights of queries whose states are joined at a time
+    static constexpr int kState = kJoined * 8 * (D + 2);        // floats of a warp's state of these
+    static constexpr int kPerSm = kRowBytes == 256 || NT == 4 ? 2 : D == 128 ? (NT == 1 ? 4 : 3) : 4;
+    static constexpr int kFixed = 2 * kState * 4 + 2 * kQueryBytes + 2 * kQueries * 4 + 24 * 4 + 1024 /* alignment */ + 256 /* barriers, notes */;
     static constexpr int kStagesThatFit = ((227 * 1024 + 1024) / kPerSm - 1024 - kFixed) / (kStageBytes + kScaleBytes);
     static constexpr int kStages = kStagesThatFit < 8 ? kStagesThatFit : 8;
     static constexpr int kSmem = kStages * (kStageBytes + kScaleBytes) + kFixed;
@@ -241,101 +270,105 @@ struct Shape {
     static __device__ __forceinline__ int key_of(int n) { return kBoxBytes == 64 ? n : (n & 1) * 4 + (n >> 1); }
 };
 
-// The tiles of a CTA's run, segment by segment.
+// A CTA's run of slots, segment by segment.
 template <int QT>
 struct Run {
-    long long left;  // tiles, the present segment's among them
-    Segment g;
+    int left;  // slots, from `at` of the present segment on
+    int at, unit, head, tile0, tile1, tiles, limit;  // limit: keys before it exist for some row of the block
     __device__ __forceinline__ void open(const AttnArgs& a) {  // what follows from unit
-        g.limit = unit_limit<QT>(a, g.unit);
-        g.tiles = (g.limit + kTileKeys - 1) / kTileKeys;
+        limit = unit_limit<QT>(a, unit);
+        tiles = (limit + kTileKeys - 1) / kTileKeys;
     }
-    __device__ __forceinline__ void close() { g.tile1 = static_cast<int>(min(static_cast<long long>(g.tiles), g.tile0 + left)); }
+    // The tiles of the present segment; false: the run ends ahead of the first.
+    __device__ __forceinline__ bool take() {
+        tile0 = max(0, at - kSwitch);
+        tile1 = min(tiles, at + left - kSwitch);
+        return tile1 > tile0;
+    }
     __device__ __forceinline__ bool next(const AttnArgs& a) {
-        left -= g.tile1 - g.tile0;
-        if (left <= 0) return false;
-        g.tile0 = 0;
-        if (++g.head == a.cache.n_kv) {
-            g.head = 0;
+        left -= tiles + kSwitch - at;
+        if (left <= kSwitch) return false;
+        at = 0;
+        if (++head == a.cache.n_kv) {
+            head = 0;
             do {
-                ++g.unit;
+                ++unit;
                 open(a);
-            } while (g.limit == 0);
+            } while (limit == 0);
         }
-        close();
-        return true;
+        return take();
     }
 };
 
-template <int THREADS>
-__device__ __forceinline__ void compute_sync() { asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory"); }
+__device__ __forceinline__ void compute_sync() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kWarps) : "memory"); }
 
-template <int D, int KV, int MT>
-__global__ void __launch_bounds__(Shape<D, KV, MT>::kThreads, Shape<D, KV, MT>::kPerSm)
+template <int D, int KV, int NT>
+__global__ void __launch_bounds__(Shape<D, KV, NT>::kThreads, Shape<D, KV, NT>::kPerSm)
 paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ AttnArgs a) {
-    using S = Shape<D, KV, MT>;
+    using S = Shape<D, KV, NT>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     float* ring_scales = reinterpret_cast<float*>(ring + S::kStages * S::kStageBytes);  // [stage][K, V][64]
-    float* merge = reinterpret_cast<float*>(ring + S::kStages * (S::kStageBytes + S::kScaleBytes));
-    uint4* q_frag = reinterpret_cast<uint4*>(merge + S::kMerge / 4);                 // [MT][D / 16][32 lanes]
-    float* q_factor = reinterpret_cast<float*>(q_frag + S::kQueryBytes / 16);  // what a row's products are multiplied with
-    long long* scratch = reinterpret_cast<long long*>(q_factor + S::kQueries);
-    uint64_t* full_bar = reinterpret_cast<uint64_t*>(scratch + 40);
+    float* merge = reinterpret_cast<float*>(ring + S::kStages * (S::kStageBytes + S::kScaleBytes));  // [2] states
+    // Queries of this and of the next segment: rows as they came, then [NT][D / 32][32 lanes] in the order in which the products take them.
+    uint8_t* queries = reinterpret_cast<uint8_t*>(merge + 2 * S::kState);
+    float* query_factor = reinterpret_cast<float*>(queries + 2 * S::kQueryBytes);  // [2][row]: what a row's products are multiplied with
+    uint64_t* full_bar = reinterpret_cast<uint64_t*>(query_factor + 2 * S::kQueries);
     uint64_t* empty_bar = full_bar + S::kStages;
     int* notes = reinterpret_cast<int*>(empty_bar + S::kStages);  // [stage]: keys of the tile that there are, and which of its halves were fetched
+    int* scratch = notes + S::kStages;                            // [24]
 
     const int warp = __shfl_sync(kFullMask, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::kStages; ++s) {
             mbar_init(&full_bar[s], 1);
-            mbar_init(&empty_bar[s], S::kComputeWarps);
+            mbar_init(&empty_bar[s], kWarps);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     pdl_wait();
     pdl_trigger();  // (behind the wait: the joining kernel reads the lengths ahead of its own)
 
-    long long total = 0, before = 0;
-    int unit = 0, ctas = 0;
-    find_unit<S::kQueries>(a, scratch, [&](long long sum) {
-        ctas = max(1, ctas_of(sum, a.grid));
-        return static_cast<int>(blockIdx.x) < ctas ? first_tile(sum, blockIdx.x, ctas) : sum;
-    }, total, unit, before);
-    if (unit < 0) return;  // (more CTAs than tiles)
+    int unit, before;
+    const Shares shares(find_unit<S::kQueries>(a, scratch, unit, before), a.grid);
+    if (unit < 0) return;  // (more CTAs than slots)
     Run<S::kQueries> run;
-    Segment& g = run.g;
     {
-        const long long first = first_tile(total, blockIdx.x, ctas), within = first - before * a.cache.n_kv;
-        run.left = first_tile(total, blockIdx.x + 1, ctas) - first;
-        g.unit = unit;
+        const int first = shares.first(blockIdx.x), within = first - before * a.cache.n_kv;
+        run.left = shares.first(blockIdx.x + 1) - first;
+        run.unit = unit;
         run.open(a);
-        g.head = static_cast<int>(within / g.tiles);
-        g.tile0 = static_cast<int>(within - static_cast<long long>(g.head) * g.tiles);
-        run.close();
+        const int slots = run.tiles + kSwitch;
+        run.head = static_cast<int>(static_cast<uint32_t>(within) / static_cast<uint32_t>(slots));
+        run.at = within - run.head * slots;
     }
+    if (!run.take()) return;
     __syncthreads();  // (barriers are there for all)
     uint32_t limit = kSpinLimit;  // of every wait; one that has run out leaves one try to the others, and the CTA ends with its error noted
 
-    if (warp == S::kComputeWarps) {
+    if (warp >= kWarps) {
+        if constexpr (S::kShift) {
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kLeft));
+            if (warp > kWarps) return;
+        }
         // ---- the tiles of the whole run, through the ring: halves of 32 keys, which lie in one page each ----
         const bool leader = elect_one();
         int stage = 0, use = 0;
         do {
-            const int b = g.unit / a.blocks;
+            const int b = a.blocks == 1 ? run.unit : run.unit / a.blocks;
             const int32_t* pages = a.cache.table + static_cast<size_t>(b) * a.cache.width;
-            for (int t = g.tile0; t < g.tile1; ++t) {
+            for (int t = run.tile0; t < run.tile1; ++t) {
                 int page[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int key = t * kTileKeys + 32 * h;
-                    page[h] = key < g.limit ? pages[key >> a.cache.page_shift] : -1;
+                    page[h] = key < run.limit ? pages[key >> a.cache.page_shift] : -1;
                     if (page[h] >= a.cache.pages) page[h] = -1;
                 }
                 if (use > 0 && !mbar_wait_warp(&empty_bar[stage], (use - 1) & 1, limit)) limit = 1;
                 if (leader) {
                     const int halves = (page[0] >= 0 ? 1 : 0) + (page[1] >= 0 ? 1 : 0);
-                    notes[stage] = min(kTileKeys, g.limit - t * kTileKeys) | (page[0] >= 0 ? 256 : 0) | (page[1] >= 0 ? 512 : 0);
+                    notes[stage] = min(kTileKeys, run.limit - t * kTileKeys) | (page[0] >= 0 ? 256 : 0) | (page[1] >= 0 ? 512 : 0);
                     mbar_expect_tx(&full_bar[stage], halves * (S::kStageBytes + S::kScaleBytes) / 2);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
@@ -343,7 +376,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                         const int slot = (t * kTileKeys + 32 * h) & ((1 << a.cache.page_shift) - 1);
 #pragma unroll
                         for (int which = 0; which < 2; ++which) {
-                            const int plane = (page[h] * 2 + which) * a.cache.n_kv + g.head;
+                            const int plane = (page[h] * 2 + which) * a.cache.n_kv + run.head;
                             uint8_t* to = ring + stage * S::kStageBytes + which * S::kOperandBytes + h * 32 * S::kBoxBytes;
 #pragma unroll
                             for (int box = 0; box < S::kBoxes; ++box)
@@ -368,300 +401,372 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
         return;
     }
 
-    const int mt = warp % MT, group = warp / MT;
+    if constexpr (S::kShift) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kTaken));
     const int r0 = lane >> 2, c = lane & 3;
-    constexpr int kCompute = 32 * S::kComputeWarps;
-    int stage = 0, use = 0;
-    do {
-        const int b = g.unit / a.blocks, block = g.unit - b * a.blocks;
-        const int length = a.lengths[b];
+    constexpr int kRows = S::kQueries / kWarps;  // queries that a warp fetches and prepares: warp, warp + 4, ..
+    const auto fetch_queries = [&](const Run<S::kQueries>& of, int turn) {
+        const int b = a.blocks == 1 ? of.unit : of.unit / a.blocks, block = of.unit - b * a.blocks;
+#pragma unroll
+        for (int j = 0; j < kRows; ++j) {
+            const int row = warp + j * kWarps, query = block * S::kQueries + row, token = a.token_of(query);
+            const bool there = token < a.rows;
+            const size_t at = (static_cast<size_t>(b) * a.rows + token) * a.q_stride + (of.head * a.group + query - token * a.group) * D + 4 * lane;
+            if (lane < D / 4) copy8(queries + turn * S::kQueryBytes + row * (2 * D) + 8 * lane, static_cast<const uint16_t*>(a.q) + (there ? at : 0), there);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    int stage = 0, use = 0, turn = 0;
+    fetch_queries(run, 0);
+    while (true) {
+        const int b = a.blocks == 1 ? run.unit : run.unit / a.blocks, block = run.unit - b * a.blocks;
+        const int length = max(a.lengths[b], 0);
+        Run<S::kQueries> ahead = run;
+        const bool more = ahead.next(a);
 
-        // ---- the block's queries, in the order in which the products take them ----
+        // ---- the block's queries ----
         // Lane c of a quad reads dims E (4 i + c) + 4 s .. + 3 of a key row (E elements to 16 bytes), so step E/4 i + s of the
         // product takes the same dims of the query.  fp16 rows are brought to a largest magnitude in [1, 2) by a power of two.
         constexpr int E = 16 / (S::kRowBytes / D), kPerChunk = E / 4;
-        for (int row = warp; row < S::kQueries; row += S::kComputeWarps) {
-            const int query = block * S::kQueries + row, i = query / a.group;
-            const bool there = i < a.rows;
+        const uint4* q_frag = reinterpret_cast<const uint4*>(queries + turn * S::kQueryBytes);
+        const float* q_factor = query_factor + turn * S::kQueries;
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncwarp();
+        uint32_t packed[kRows][2];
+#pragma unroll
+        for (int j = 0; j < kRows; ++j) {
+            const int row = warp + j * kWarps;
             float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (there && lane < D / 4) {
-                const int head = g.head * a.group + query - i * a.group;
-                const size_t at = (static_cast<size_t>(b) * a.rows + i) * a.q_stride + head * D + 4 * lane;
-                if (a.q_bf16) load_row(static_cast<const __nv_bfloat16*>(a.q) + at, true, v);
-                else load_row(static_cast<const __half*>(a.q) + at, true, v);
+            if (lane < D / 4) {
+                const uint8_t* from = queries + turn * S::kQueryBytes + row * (2 * D) + 8 * lane;
+                if (a.q_bf16) load_row(reinterpret_cast<const __nv_bfloat16*>(from), true, v);
+                else load_row(reinterpret_cast<const __half*>(from), true, v);
             }
             float back = 1.0f;
             if constexpr (!S::kBf16) {
                 uint32_t largest = 0u;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) largest = max(largest, magnitude(v[j]));
+                for (int i = 0; i < 4; ++i) largest = max(largest, magnitude(v[i]));
                 largest = __reduce_max_sync(kFullMask, largest);
                 if (largest != 0u && largest < 0x7f800000u) {
                     const int e = max(-120, min(120, static_cast<int>(largest >> 23) - 127));
                     back = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
                     const float by = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] *= by;
+                    for (int i = 0; i < 4; ++i) v[i] *= by;
                 }
             }
-            if (lane < D / 4) {
-                const int dim = 4 * lane, chunk = dim / E, step = (chunk >> 2) * kPerChunk + (dim % E) / 4;
-                uint32_t* to = reinterpret_cast<uint32_t*>(q_frag + ((row >> 4) * (D / 16) + step) * 32 + (row & 7) * 4 + (chunk & 3)) + ((row >> 3) & 1);
-                to[0] = pack2<S::kBf16>(v[0], v[1]);
-                to[2] = pack2<S::kBf16>(v[2], v[3]);
-            }
-            if (lane == 0) q_factor[row] = back * a.scale * kLog2e;
+            packed[j][0] = pack2<S::kBf16>(v[0], v[1]);
+            packed[j][1] = pack2<S::kBf16>(v[2], v[3]);
+            if (lane == 0) query_factor[turn * S::kQueries + row] = back * a.scale * kLog2e;
         }
-        compute_sync<kCompute>();
-
-        // positions of this thread's two queries; one that does not exist sees nothing
-        int seen[2];
+        compute_sync();  // (all rows are in registers: their place takes them in the other order)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int i = (block * S::kQueries + mt * 16 + r0 + 8 * h) / a.group;
-            seen[h] = i < a.rows ? static_cast<int>(max(-1ll, static_cast<long long>(length) - a.rows + i)) : -1;
+        for (int j = 0; j < kRows; ++j) {
+            const int row = warp + j * kWarps, dim = 4 * lane, chunk = dim / E, step = (chunk >> 2) * kPerChunk + (dim % E) / 4;
+            if (lane < D / 4)
+                *reinterpret_cast<uint2*>(queries + turn * S::kQueryBytes + (((row >> 3) * (D / 32) + (step >> 1)) * 32 + (row & 7) * 4 + (chunk & 3)) * 16 + (step & 1) * 8) =
+                    make_uint2(packed[j][0], packed[j][1]);
         }
-        const int seen_by_all = static_cast<int>(max(-1ll, static_cast<long long>(length) - a.rows + min(a.rows - 1, block * S::kQueries / a.group)));
-        const float factor[2] = {q_factor[mt * 16 + r0], q_factor[mt * 16 + r0 + 8]};
+        compute_sync();
+        if (more) fetch_queries(ahead, turn ^ 1);  // (the place of the segment before: all warps are behind its products)
 
-        float o[D / 8][4], top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.0f, 0.0f};
-#pragma unroll
-        for (int n = 0; n < D / 8; ++n)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) o[n][j] = 0.0f;
+        // (this thread's queries: 8 n + 2 c and the next, of each eight n)
+        const int seen_by_all = max(-1, length - a.rows + min(a.rows - 1, a.token_of(block * S::kQueries)));
 
-        for (int t = g.tile0; t < g.tile1; ++t) {
+        float o[NT][D / 16][4], top[NT][2], sum[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int m = 0; m < D / 16; ++m)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[n][m][j] = 0.0f;
+            top[n][0] = top[n][1] = -INFINITY;
+            sum[n][0] = sum[n][1] = 0.0f;
+        }
+
+        for (int t = run.tile0; t < run.tile1; ++t) {
             if (!mbar_wait_warp(&full_bar[stage], use & 1, limit)) limit = 1;
             const uint8_t* keys = ring + stage * S::kStageBytes;
             uint8_t* values = ring + stage * S::kStageBytes + S::kOperandBytes;
-            const float* consts = ring_scales + stage * 2 * kTileKeys;
+            const float* consts = ring_scales + stage * 2 * kTileKeys + warp * 16;
             const int note = notes[stage];
             // keys of this warp's sixteen that there are (they lie in one half of the tile)
-            const int there = note & (group >= kGroups / 2 ? 512 : 256) ? max(0, min(16, (note & 255) - 16 * group)) : 0;
-            const int first_key = t * kTileKeys + group * 16;
+            const int there = note & (warp >= kWarps / 2 ? 512 : 256) ? max(0, min(16, (note & 255) - 16 * warp)) : 0;
+            const int first_key = t * kTileKeys + warp * 16;
 
             // A weight of zero does not hide a V row that is no number from the product.  Rows that are not there (left from
             // before, or of other sequences) are cleared; rows that some of the block's queries see and others do not are looked at,
             // and one with such a value is taken out and told to those who see it.
-            const bool hidden = KV != SPEC_DTYPE_INT8 && first_key + 15 > seen_by_all && seen_by_all + 1 < g.limit;
+            const bool hidden = KV != SPEC_DTYPE_INT8 && first_key + 15 > seen_by_all && seen_by_all + 1 < run.limit;
             uint32_t bad = 0u;  // a bit per key
             if (KV != SPEC_DTYPE_INT8 && (there < 16 || hidden)) {
                 if (hidden) {
                     for (int i = lane; i < 16 * S::kChunks; i += 32) {
                         const int r = i / S::kChunks;
-                        if (r < there && not_numbers<KV>(*reinterpret_cast<const uint4*>(values + S::place(group * 16 + r, i % S::kChunks)))) bad |= 1u << r;
+                        if (r < there && not_numbers<KV>(*reinterpret_cast<const uint4*>(values + S::place(warp * 16 + r, i % S::kChunks)))) bad |= 1u << r;
                     }
                     bad = __reduce_or_sync(kFullMask, bad);
-                    // (the warps with the same keys look before one of them clears)
-                    if constexpr (MT > 1) asm volatile("bar.sync %0, %1;" ::"r"(2 + group), "n"(32 * MT) : "memory");
                 }
                 for (int i = lane; i < 16 * S::kChunks; i += 32) {
                     const int r = i / S::kChunks;
-                    if (r >= there || (bad >> r & 1u)) *reinterpret_cast<uint4*>(values + S::place(group * 16 + r, i % S::kChunks)) = make_uint4(0u, 0u, 0u, 0u);
+                    if (r >= there || (bad >> r & 1u)) *reinterpret_cast<uint4*>(values + S::place(warp * 16 + r, i % S::kChunks)) = make_uint4(0u, 0u, 0u, 0u);
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // (before the next copy into this stage)
+                __syncwarp();
             }
-            float s[2][4];
+
+            // ---- scores: this thread's keys are key[0], key[1] ----
+            const int key[2] = {S::key_of(r0), 8 + S::key_of(r0)};
+            float s[NT][4];
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) s[n][j] = 0.0f;
-            const uint4* queries = q_frag + mt * (D / 16) * 32 + lane;
 #pragma unroll
             for (int i = 0; i < S::kChunks / 4; ++i) {
+                uint32_t w[2][4];
 #pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    const uint4 w = *reinterpret_cast<const uint4*>(keys + S::place(group * 16 + n * 8 + S::key_of(r0), 4 * i + c));
-                    if constexpr (S::kEight) {
-                        const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+                for (int h = 0; h < 2; ++h) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(keys + S::place(warp * 16 + key[h], 4 * i + c));
+                    w[h][0] = v.x;
+                    w[h][1] = v.y;
+                    w[h][2] = v.z;
+                    w[h][3] = v.w;
+                }
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            uint32_t b0, b1;
-                            widen<KV, 1>(words[k], b0, b1);
-                            mma16816<S::kBf16>(s[n], queries[(4 * i + k) * 32], b0, b1);
+                for (int k = 0; k < kPerChunk; k += 2) {
+                    uint4 rows[2];  // of K, for two steps
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        if constexpr (S::kEight) {
+                            widen<KV, 1>(w[0][k + e], rows[e].x, rows[e].z);
+                            widen<KV, 1>(w[1][k + e], rows[e].y, rows[e].w);
+                        } else {
+                            rows[e] = make_uint4(w[0][2 * e], w[1][2 * e], w[0][2 * e + 1], w[1][2 * e + 1]);
                         }
-                    } else {
-                        mma16816<S::kBf16>(s[n], queries[(2 * i) * 32], w.x, w.y);
-                        mma16816<S::kBf16>(s[n], queries[(2 * i + 1) * 32], w.z, w.w);
+                    }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const uint4 q = q_frag[(n * (D / 32) + (kPerChunk * i + k) / 2) * 32 + lane];
+                        mma16816<S::kBf16>(s[n], rows[0], q.x, q.y);
+                        mma16816<S::kBf16>(s[n], rows[1], q.z, q.w);
                     }
                 }
             }
             // ---- exponents, their running maximum, weights ----
-            float inv[2][2];
-            float now[2] = {-INFINITY, -INFINITY};
+            float inv[2] = {1.0f, 1.0f};
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
+            for (int h = 0; h < 2; ++h) {
+                float sk = 1.0f, raise = 0.0f;  // (the queries' factors are loaded anew for each tile: they would be two registers each)
+                if constexpr (S::kEight) {
+                    const float sv = consts[kTileKeys + key[h]];
+                    sk = consts[key[h]];
+                    raise = log2_of(sv);
+                    inv[h] = reciprocal_of(sv);
+                }
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    inv[n][x] = 1.0f;
+                for (int n = 0; n < NT; ++n) {
+                    const float2 factor = *reinterpret_cast<const float2*>(q_factor + 8 * n + 2 * c);
                     if constexpr (S::kEight) {
-                        const int key = group * 16 + n * 8 + S::key_of(2 * c + x);
-                        const float sk = consts[key], sv = consts[kTileKeys + key], raise = log2_of(sv);
-                        inv[n][x] = reciprocal_of(sv);
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) s[n][2 * h + x] = fmaf(s[n][2 * h + x], sk * factor[h], raise);
+                        s[n][2 * h] = fmaf(s[n][2 * h], sk * factor.x, raise);
+                        s[n][2 * h + 1] = fmaf(s[n][2 * h + 1], sk * factor.y, raise);
                     } else {
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) s[n][2 * h + x] *= factor[h];
+                        s[n][2 * h] *= factor.x;
+                        s[n][2 * h + 1] *= factor.y;
                     }
                 }
+            }
             if (there < 16 || first_key + 15 > seen_by_all) {  // keys that are not there, or not for every query
+                bool number[2];
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
+                for (int h = 0; h < 2; ++h) {
+                    number[h] = !(bad >> key[h] & 1u);
+                    if constexpr (S::kEight) number[h] = number[h] && magnitude(consts[kTileKeys + key[h]]) < 0x7f800000u;
+                    // (a row of V that is no number makes the exponent none for who sees it, and no one else's sum)
+                    if (!number[h] || key[h] >= there) inv[h] = 0.0f;
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        const int key = n * 8 + S::key_of(2 * c + x);
-                        bool number = !(bad >> key & 1u);
-                        if constexpr (S::kEight) number = number && magnitude(consts[kTileKeys + group * 16 + key]) < 0x7f800000u;
-                        // (a row of V that is no number makes the exponent none for who sees it, and no one else's sum)
-                        if (!number || key >= there) inv[n][x] = 0.0f;
+                        const int i = a.token_of(block * S::kQueries + 8 * n + 2 * c + x);
+                        const int seen = i < a.rows ? max(-1, length - a.rows + i) : -1;  // (a query that does not exist sees nothing)
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             float& e = s[n][2 * h + x];
-                            if (!number) e = NAN;
-                            if (key >= there || first_key + key > seen[h]) e = -INFINITY;
+                            if (!number[h]) e = NAN;
+                            if (key[h] >= there || first_key + key[h] > seen) e = -INFINITY;
                         }
                     }
             }
+            float now[NT][2];
+            bool higher = false;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) now[h] = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                now[h] = fmaxf(now[h], __shfl_xor_sync(kFullMask, now[h], 1));
-                now[h] = fmaxf(now[h], __shfl_xor_sync(kFullMask, now[h], 2));
+                for (int x = 0; x < 2; ++x) now[n][x] = fmaxf(s[n][x], s[n][2 + x]);
+#pragma unroll
+            for (int lanes = 4; lanes < 32; lanes <<= 1)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) now[n][x] = fmaxf(now[n][x], __shfl_xor_sync(kFullMask, now[n][x], lanes));
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) higher = higher || now[n][x] > top[n][x] + kSlack;
+            if (__any_sync(kFullMask, higher)) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    float shrink[2];
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const float most = fmaxf(top[n][x], now[n][x]);
+                        shrink[x] = top[n][x] == -INFINITY ? 0.0f : exp2_of(top[n][x] - most);
+                        top[n][x] = most;
+                        sum[n][x] *= shrink[x];
+                    }
+#pragma unroll
+                    for (int m = 0; m < D / 16; ++m)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) o[n][m][j] *= shrink[j & 1];
+                }
             }
-            if (__any_sync(kFullMask, now[0] > top[0] + kSlack || now[1] > top[1] + kSlack)) {
-                float shrink[2];
+            uint32_t p[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const float higher = fmaxf(top[h], now[h]);
-                    shrink[h] = top[h] == -INFINITY ? 0.0f : exp2_of(top[h] - higher);
-                    top[h] = higher;
-                    sum[h] *= shrink[h];
-                }
 #pragma unroll
-                for (int n = 0; n < D / 8; ++n) {
-                    o[n][0] *= shrink[0];
-                    o[n][1] *= shrink[0];
-                    o[n][2] *= shrink[1];
-                    o[n][3] *= shrink[1];
-                }
-            }
-            uint4 p;
-            {
-                const float from[2] = {top[0] == -INFINITY ? 0.0f : top[0], top[1] == -INFINITY ? 0.0f : top[1]};
-#pragma unroll
-                for (int n = 0; n < 2; ++n)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        s[n][j] = exp2_of(s[n][j] - from[j >> 1]);
-                        sum[j >> 1] = fmaf(s[n][j], inv[n][j & 1], sum[j >> 1]);
+                    for (int x = 0; x < 2; ++x) {
+                        const float w = exp2_of(s[n][2 * h + x] - (top[n][x] == -INFINITY ? 0.0f : top[n][x]));
+                        sum[n][x] = fmaf(w, inv[h], sum[n][x]);
+                        s[n][2 * h + x] = w;
                     }
-                p.x = pack2<S::kBf16>(s[0][0], s[0][1]);
-                p.y = pack2<S::kBf16>(s[0][2], s[0][3]);
-                p.z = pack2<S::kBf16>(s[1][0], s[1][1]);
-                p.w = pack2<S::kBf16>(s[1][2], s[1][3]);
+                    p[n][h] = transposed(pack2<S::kBf16>(s[n][2 * h], s[n][2 * h + 1]));
+                }
             }
-            // ---- weights times values: key 2 c, 2 c + 1 (and + 8) of the product are the columns of the scores ----
+            // ---- values times weights: rows of V in the order of the keys above ----
             const uint32_t v_base = smem_u32(values);
-            const int v_row = group * 16 + ((lane >> 3) & 1) * 8 + S::key_of(lane & 7);
+            const int v_row = warp * 16 + ((lane >> 3) & 1) * 8 + S::key_of(lane & 7);
 #pragma unroll
             for (int i = 0; i < S::kChunks / 2; ++i) {
-                uint32_t w[4];
+                uint32_t w[4];  // two chunks of eight keys, twice
                 ldmatrix4_trans(w, v_base + S::place(v_row, 2 * i + (lane >> 4)));
+                if constexpr (S::kEight) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if constexpr (S::kEight) {
-                        uint32_t even0, odd0, even1, odd1;
-                        widen<KV, 2>(w[2 * h], even0, odd0);
-                        widen<KV, 2>(w[2 * h + 1], even1, odd1);
-                        mma16816<S::kBf16>(o[2 * (2 * i + h)], p, even0, even1);
-                        mma16816<S::kBf16>(o[2 * (2 * i + h) + 1], p, odd0, odd1);
-                    } else {
-                        mma16816<S::kBf16>(o[2 * i + h], p, w[2 * h], w[2 * h + 1]);
+                    for (int h = 0; h < 2; ++h) {  // a chunk is sixteen dims: the even ones are rows 0 .. 7 of the product, the odd ones 8 .. 15
+                        uint4 v;
+                        widen<KV, 2>(w[2 * h], v.x, v.y);
+                        widen<KV, 2>(w[2 * h + 1], v.z, v.w);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) mma16816<S::kBf16>(o[n][2 * i + h], v, p[n][0], p[n][1]);
                     }
+                } else {
+                    const uint4 v = make_uint4(w[0], w[2], w[1], w[3]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) mma16816<S::kBf16>(o[n][i], v, p[n][0], p[n][1]);
                 }
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&empty_bar[stage]);
             if (++stage == S::kStages) { stage = 0; ++use; }
         }
+        // ---- the four warps' states become one: warps 2, 3 into 0, 1, then 1 into 0 ----
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            sum[h] += __shfl_xor_sync(kFullMask, sum[h], 1);
-            sum[h] += __shfl_xor_sync(kFullMask, sum[h], 2);
-        }
-        // ---- the four groups' states become one: groups 2, 3 into 0, 1, then 1 into 0 ----
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int step = kGroups / 2; step > 0; step >>= 1) {
-            compute_sync<kCompute>();  // (whoever read the place before is done)
-            if (group >= step && group < 2 * step) {
-                float* to = merge + ((group - step) * MT + mt) * 16 * (D + 2) + lane;
+            for (int x = 0; x < 2; ++x)
 #pragma unroll
-                for (int n = 0; n < D / 8; ++n)
+                for (int lanes = 4; lanes < 32; lanes <<= 1) sum[n][x] += __shfl_xor_sync(kFullMask, sum[n][x], lanes);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) to[(n * 4 + j) * 32] = o[n][j];
-                if (c == 0) {
-                    float* ml = merge + ((group - step) * MT + mt) * 16 * (D + 2) + 16 * D;
-                    ml[r0] = top[0];
-                    ml[r0 + 8] = top[1];
-                    ml[16 + r0] = sum[0];
-                    ml[16 + r0 + 8] = sum[1];
-                }
-            }
-            compute_sync<kCompute>();
-            if (group < step) {
-                const float* from = merge + (group * MT + mt) * 16 * (D + 2);
-                float keep[2], take[2];
+        for (int n0 = 0; n0 < NT; n0 += S::kJoined) {
+            constexpr int kElements = D / 16 * 4 * 32;  // of eight queries
+            const auto leave = [&](float* to) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float other = from[16 * D + r0 + 8 * h], higher = fmaxf(top[h], other);
-                    keep[h] = top[h] == -INFINITY ? 0.0f : exp2_of(top[h] - higher);
-                    take[h] = other == -INFINITY ? 0.0f : exp2_of(other - higher);
-                    sum[h] = sum[h] * keep[h] + from[16 * D + 16 + r0 + 8 * h] * take[h];
-                    top[h] = higher;
-                }
+                for (int n = 0; n < S::kJoined; ++n) {
 #pragma unroll
-                for (int n = 0; n < D / 8; ++n)
+                    for (int m = 0; m < D / 16; ++m)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) o[n][j] = o[n][j] * keep[j >> 1] + from[lane + (n * 4 + j) * 32] * take[j >> 1];
-            }
-        }
-        if (group == 0) {
-            const bool whole = g.tile0 == 0 && g.tile1 == g.tiles;
-            const long long slot = static_cast<long long>(blockIdx.x) + static_cast<long long>(g.unit) * a.cache.n_kv + g.head;
+                        for (int j = 0; j < 4; ++j) to[n * kElements + (m * 4 + j) * 32 + lane] = o[n0 + n][m][j];
+                    if (r0 == 0) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int row = mt * 16 + r0 + 8 * h, query = block * S::kQueries + row, i = query / a.group;
-                if (i >= a.rows) continue;
-                const float by = whole ? (sum[h] == 0.0f ? 0.0f : __fdividef(1.0f, sum[h])) : 1.0f;
-                const size_t at = ((static_cast<size_t>(b) * a.rows + i) * a.n_heads + g.head * a.group + query - i * a.group) * D;
-                float* part = a.partial + (slot * S::kQueries + row) * D;
-                if (!whole && c == 0) a.partial_ml[slot * S::kQueries + row] = make_float2(top[h], sum[h]);
-#pragma unroll
-                for (int n = 0; n < D / 8; n += 2) {
-                    // 8-bit rows: tiles n, n + 1 hold the even and the odd dims of 16; 16-bit rows: 8 dims each
-                    if constexpr (S::kEight) {
-                        const float v[4] = {o[n][2 * h] * by, o[n + 1][2 * h] * by, o[n][2 * h + 1] * by, o[n + 1][2 * h + 1] * by};
-                        const int dim = 8 * n + 4 * c;
-                        if (!whole) *reinterpret_cast<float4*>(part + dim) = *reinterpret_cast<const float4*>(v);
-                        else if (a.q_bf16) store_row(static_cast<__nv_bfloat16*>(a.out) + at + dim, true, v);
-                        else store_row(static_cast<__half*>(a.out) + at + dim, true, v);
-                    } else {
-#pragma unroll
-                        for (int m = 0; m < 2; ++m) {
-                            const int dim = 8 * (n + m) + 2 * c;
-                            const float x = o[n + m][2 * h] * by, y = o[n + m][2 * h + 1] * by;
-                            if (!whole) *reinterpret_cast<float2*>(part + dim) = make_float2(x, y);
-                            else if (a.q_bf16) *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(a.out) + at + dim) = pack2<true>(x, y);
-                            else *reinterpret_cast<uint32_t*>(static_cast<__half*>(a.out) + at + dim) = pack2<false>(x, y);
+                        for (int x = 0; x < 2; ++x) {
+                            to[S::kJoined * kElements + 16 * n + 2 * c + x] = top[n0 + n][x];
+                            to[S::kJoined * kElements + 16 * n + 8 + 2 * c + x] = sum[n0 + n][x];
                         }
                     }
                 }
-            }
+            };
+            const auto join = [&](const float* from) {
+#pragma unroll
+                for (int n = 0; n < S::kJoined; ++n) {
+                    float keep[2], take[2];
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        float &mine = top[n0 + n][x], other = from[S::kJoined * kElements + 16 * n + 2 * c + x];
+                        const float most = fmaxf(mine, other);
+                        keep[x] = mine == -INFINITY ? 0.0f : exp2_of(mine - most);
+                        take[x] = other == -INFINITY ? 0.0f : exp2_of(other - most);
+                        sum[n0 + n][x] = sum[n0 + n][x] * keep[x] + from[S::kJoined * kElements + 16 * n + 8 + 2 * c + x] * take[x];
+                        mine = most;
+                    }
+#pragma unroll
+                    for (int m = 0; m < D / 16; ++m)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            o[n0 + n][m][j] = o[n0 + n][m][j] * keep[j & 1] + from[n * kElements + (m * 4 + j) * 32 + lane] * take[j & 1];
+                }
+            };
+            if (n0 > 0) compute_sync();  // (warp 0 has read the second place)
+            if (warp >= 2) leave(merge + (warp - 2) * S::kState);
+            compute_sync();
+            if (warp < 2) join(merge + warp * S::kState);
+            if (warp == 1) leave(merge + S::kState);
+            compute_sync();
+            if (warp == 0) join(merge + S::kState);
         }
-        compute_sync<kCompute>();  // (the queries' place is free for the next segment's)
-    } while (run.next(a));
+        if (warp == 0) {
+            const bool whole = run.tile0 == 0 && run.tile1 == run.tiles;
+            const size_t slot = static_cast<size_t>(blockIdx.x) + static_cast<size_t>(run.unit) * a.cache.n_kv + run.head;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int row = 8 * n + 2 * c + x, query = block * S::kQueries + row, i = a.token_of(query);
+                    if (i >= a.rows) continue;
+                    const float by = whole ? (sum[n][x] == 0.0f ? 0.0f : reciprocal_of(sum[n][x])) : 1.0f;
+                    const size_t at = ((static_cast<size_t>(b) * a.rows + i) * a.n_heads + run.head * a.group + query - i * a.group) * D;
+                    float* part = a.partial + (slot * S::kQueries + row) * D;
+                    if (!whole && r0 == 0) a.partial_ml[slot * S::kQueries + row] = make_float2(top[n][x], sum[n][x]);
+#pragma unroll
+                    for (int m = 0; m < D / 16; ++m) {
+                        const float u = o[n][m][x] * by, v = o[n][m][2 + x] * by;
+                        if constexpr (S::kEight) {  // dims 2 r0 and the next
+                            const int dim = 16 * m + 2 * r0;
+                            if (!whole) *reinterpret_cast<float2*>(part + dim) = make_float2(u, v);
+                            else if (a.q_bf16) *reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(a.out) + at + dim) = pack2<true>(u, v);
+                            else *reinterpret_cast<uint32_t*>(static_cast<__half*>(a.out) + at + dim) = pack2<false>(u, v);
+                        } else {  // dims r0 and r0 + 8
+                            const int dim = 16 * m + r0;
+                            if (!whole) {
+                                part[dim] = u;
+                                part[dim + 8] = v;
+                            } else if (a.q_bf16) {
+                                static_cast<__nv_bfloat16*>(a.out)[at + dim] = __float2bfloat16_rn(u);
+                                static_cast<__nv_bfloat16*>(a.out)[at + dim + 8] = __float2bfloat16_rn(v);
+                            } else {
+                                static_cast<__half*>(a.out)[at + dim] = __float2half_rn(u);
+                                static_cast<__half*>(a.out)[at + dim + 8] = __float2half_rn(v);
+                            }
+                        }
+                    }
+                }
+        }
+        if (!more) break;
+        run = ahead;
+        turn ^= 1;
+    }
     if (limit != kSpinLimit && lane == 0) atomicCAS(&g_paged_error, 0, 2);
 }
 
@@ -672,29 +777,26 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
 template <int D, int QT, int SHARE>
 __global__ void __launch_bounds__(128)
 join_kernel(const __grid_constant__ AttnArgs a) {
-    constexpr int kPer = D / 32, kBatch = 8, kWarps = 4;
-    __shared__ long long counts[2 * kWarps];
+    constexpr int kPer = D / 32, kBatch = 8;
+    __shared__ int counts[2 * kWarps];
     __shared__ float states[SHARE][D + 2];
     pdl_trigger();
     const int unit = blockIdx.x / a.cache.n_kv, head = blockIdx.x - unit * a.cache.n_kv;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int b = unit / a.blocks, block = unit - b * a.blocks;
-    const int row = blockIdx.y * (kWarps / SHARE) + warp / SHARE, query = block * QT + row, i = query / a.group;
+    const int b = a.blocks == 1 ? unit : unit / a.blocks, block = unit - b * a.blocks;
+    const int row = blockIdx.y * (kWarps / SHARE) + warp / SHARE, query = block * QT + row, i = a.token_of(query);
     // (the lengths may be read ahead of the wait: the kernel in front lets this one start behind its own wait only)
     const int limit = unit_limit<QT>(a, unit), tiles = (limit + kTileKeys - 1) / kTileKeys;
-    long long total = 0, front = 0;
-    {  // tiles of all units, and of those before this one
-        long long all = 0, mine = 0;
+    int total = 0, front = 0;
+    {  // slots of all units, and those before this segment's first tile
+        int all = 0, mine = 0;
         for (int u = threadIdx.x; u < a.units; u += 32 * kWarps) {
-            const int n = (unit_limit<QT>(a, u) + kTileKeys - 1) / kTileKeys;
+            const int n = unit_slots(unit_limit<QT>(a, u));
             all += n;
             if (u < unit) mine += n;
         }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            all += __shfl_xor_sync(kFullMask, all, o);
-            mine += __shfl_xor_sync(kFullMask, mine, o);
-        }
+        all = __reduce_add_sync(kFullMask, all);
+        mine = __reduce_add_sync(kFullMask, mine);
         if (lane == 0) {
             counts[warp] = all;
             counts[kWarps + warp] = mine;
@@ -705,16 +807,21 @@ join_kernel(const __grid_constant__ AttnArgs a) {
             front += counts[kWarps + w];
         }
         total *= a.cache.n_kv;
-        front = front * a.cache.n_kv + static_cast<long long>(head) * tiles;
+        front = front * a.cache.n_kv + head * (tiles + kSwitch) + kSwitch;
     }
     if (row >= QT || i >= a.rows) return;
+    int first = 0, last = 0;
+    if (tiles > 0) {
+        const Shares shares(total, a.grid);
+        first = shares.owner(front);
+        last = shares.owner(front + tiles - 1);
+        if (first == last) return;  // (written by the CTA that has all of it)
+    }
     pdl_wait();
     const size_t at = ((static_cast<size_t>(b) * a.rows + i) * a.n_heads + head * a.group + query - i * a.group) * D;
     float v[kPer] = {}, top = -INFINITY, sum = 0.0f;
     if (tiles > 0) {
-        const int ctas = ctas_of(total, a.grid), first = owner_of(total, front, ctas), last = owner_of(total, front + tiles - 1, ctas);
-        if (first == last) return;  // (written by the CTA that had all of it)
-        const long long slot0 = static_cast<long long>(unit) * a.cache.n_kv + head;
+        const size_t slot0 = static_cast<size_t>(unit) * a.cache.n_kv + head;
         for (int p0 = first + warp % SHARE; p0 <= last; p0 += SHARE * kBatch) {
             float2 ml[kBatch];
             float part[kBatch][kPer];
@@ -778,9 +885,11 @@ join_kernel(const __grid_constant__ AttnArgs a) {
     }
 }
 
-// 16-query tiles of a block: two where the queries of a (sequence, KV head) are more than sixteen.  (Four do not fit: sixteen
-// warps and the one that fetches leave 96 registers to a thread, and 64 of them are the weighted sum.)
-int query_tiles(int rows, int group) { return static_cast<long long>(rows) * group <= 16 ? 1 : 2; }
+// Queries of a block, in eights: as many as those of a (sequence, KV head) fill, at most four.
+int query_eights(int rows, int group) {
+    const int queries = rows * group;
+    return queries <= 8 ? 1 : queries <= 16 ? 2 : 4;
+}
 
 size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
 
@@ -795,18 +904,27 @@ int rows_map(const AttnArgs& a, bool eight, int d, int box_bytes, CUtensorMap* o
                       box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, out);
 }
 
-template <int D, int KV, int MT>
+template <int D, int KV, int NT>
 int launch(const AttnArgs& args, cudaStream_t stream) {
-    using S = Shape<D, KV, MT>;
+    using S = Shape<D, KV, NT>;
     static std::atomic<unsigned long long> configured{0};
-    int status = allow_shared_memory(configured, paged_attention_kernel<D, KV, MT>, S::kSmem);
+    int status = once_on_this_device(configured, []() -> int {
+        const auto kernel = paged_attention_kernel<D, KV, NT>;
+        SPEC_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));
+        if (S::kShift) {  // (a thread that takes registers waits until its block has them: never, were the launch's too few)
+            cudaFuncAttributes f;
+            SPEC_CUDA_TRY(cudaFuncGetAttributes(&f, kernel));
+            if (f.numRegs * S::kThreads < 32 * kWarps * (S::kTaken + S::kLeft)) return fail(SPEC_ERR_CUDA, "spec_paged_attention: built with %d registers a thread", f.numRegs);
+        }
+        return SPEC_OK;
+    });
     if (status != SPEC_OK) return status;
     AttnArgs a = args;
     a.grid = 148 * S::kPerSm;
     CUtensorMap map;
     status = rows_map(a, S::kEight, D, S::kBoxBytes, &map);
     if (status != SPEC_OK) return status;
-    status = launch_pdl(paged_attention_kernel<D, KV, MT>, dim3(a.grid), dim3(S::kThreads), S::kSmem, stream, map, a);
+    status = launch_pdl(paged_attention_kernel<D, KV, NT>, dim3(a.grid), dim3(S::kThreads), S::kSmem, stream, map, a);
     if (status != SPEC_OK) return status;
     const int segments = a.units * a.cache.n_kv, queries = static_cast<int>(std::min<long long>(S::kQueries, static_cast<long long>(a.rows) * a.group));
     if (segments * 4 <= a.grid) return launch_pdl(join_kernel<D, S::kQueries, 4>, dim3(segments, queries), dim3(128), 0, stream, a);
@@ -815,7 +933,8 @@ int launch(const AttnArgs& args, cudaStream_t stream) {
 
 template <int D, int KV>
 int launch_tiles(const AttnArgs& a, cudaStream_t stream) {
-    return query_tiles(a.rows, a.group) == 1 ? launch<D, KV, 1>(a, stream) : launch<D, KV, 2>(a, stream);
+    const int eights = query_eights(a.rows, a.group);
+    return eights == 1 ? launch<D, KV, 1>(a, stream) : eights == 2 ? launch<D, KV, 2>(a, stream) : launch<D, KV, 4>(a, stream);
 }
 
 template <int D>
@@ -830,7 +949,8 @@ int launch_kv(const AttnArgs& a, int kv_dtype, cudaStream_t stream) {
 
 bool fits(int batch, int rows, int n_heads, int n_kv_heads, int d_head) {
     return batch >= 1 && batch <= 65535 && rows >= 1 && rows <= 65536 && n_kv_heads >= 1 && n_kv_heads <= 1024 && n_heads >= n_kv_heads &&
-           n_heads % n_kv_heads == 0 && n_heads <= 65536 && (d_head == 64 || d_head == 128);
+           n_heads % n_kv_heads == 0 && n_heads / n_kv_heads <= 1024 &&
+           static_cast<long long>(rows) * (n_heads / n_kv_heads) <= 1 << 20 && (d_head == 64 || d_head == 128);
 }
 long long units_of(int batch, int rows, int group, int queries) { return static_cast<long long>(batch) * ((static_cast<long long>(rows) * group + queries - 1) / queries); }
 
@@ -848,7 +968,7 @@ int paged_attention_take_error() {
 extern "C" size_t spec_paged_attention_workspace_bytes(int batch, int rows, int n_heads, int n_kv_heads, int d_head) {
     using namespace spec;
     if (!fits(batch, rows, n_heads, n_kv_heads, d_head)) return 0;
-    const int group = n_heads / n_kv_heads, queries = 16 * query_tiles(rows, group);
+    const int group = n_heads / n_kv_heads, queries = 8 * query_eights(rows, group);
     const size_t slots = kMostCtas + static_cast<size_t>(units_of(batch, rows, group, queries)) * n_kv_heads;
     return align256(slots * queries * d_head * 4) + align256(slots * queries * 8);
 }
@@ -873,9 +993,11 @@ extern "C" int spec_paged_attention(const void* q, int dtype, int64_t q_stride, 
     if (scales && !aligned_to(scales, 16)) return fail(SPEC_ERR_BAD_ARG, "%s: scales have to start on 16 bytes", who);
     if (static_cast<long long>(pages) * 2 * n_kv_heads > 0x7fffffffll) return fail(SPEC_ERR_BAD_ARG, "%s: pages=%d", who, pages);
     a.group = n_heads / n_kv_heads;
-    const int queries = 16 * query_tiles(rows, a.group);
+    const int queries = 8 * query_eights(rows, a.group);
     const long long units = units_of(batch, rows, a.group, queries);
-    if (units * n_kv_heads > 0x7fffffff - kMostCtas) return fail(SPEC_ERR_BAD_ARG, "%s: too many rows for one call", who);
+    // (slots are counted in 32 bits, with room for a CTA's share on top)
+    const long long slots_each = (static_cast<long long>(max_pages) * page_size + kTileKeys - 1) / kTileKeys + kSwitch;
+    if (units * n_kv_heads > (1ll << 30) / slots_each) return fail(SPEC_ERR_BAD_ARG, "%s: too many rows for one call", who);
     if (!workspace || workspace_bytes < spec_paged_attention_workspace_bytes(batch, rows, n_heads, n_kv_heads, d_head) || !aligned_to(workspace, 256))
         return fail(SPEC_ERR_BAD_ARG, "%s: workspace missing, too small or not 256-byte aligned", who);
     const size_t slots = kMostCtas + static_cast<size_t>(units) * n_kv_heads;
@@ -894,6 +1016,7 @@ extern "C" int spec_paged_attention(const void* q, int dtype, int64_t q_stride, 
     a.units = static_cast<int>(units);
     a.blocks = a.units / batch;
     a.q_bf16 = dtype == SPEC_DTYPE_BF16;
+    a.by_group = a.group > 1 ? static_cast<uint32_t>((0xffffffffull + a.group) / a.group) : 0u;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return d_head == 64 ? launch_kv<64>(a, kv_dtype, st) : launch_kv<128>(a, kv_dtype, st);
 }
