@@ -35,6 +35,7 @@ constexpr int kWarps = 4;        // that compute, with 16 of a tile's keys each
 constexpr int kMostCtas = 148 * 4;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kSwitch = 3;       // tiles that taking up another segment costs about as much as
+constexpr float kNone = -3.0e38f;  // the running maximum where no key has been seen: finite, so that differences stay numbers
 constexpr float kSlack = 8.0f;   // the running maximum may lag by this: w <= 2^8 stays in fp16's range
 
 __device__ int g_paged_error;  // set when the bounded wait for a tile or for its place ran out (0 = none)
@@ -253,7 +254,10 @@ struct Shape {
     static constexpr int kQueryBytes = kQueries * D * 2;
     static constexpr int kJoined = NT < 2 ? NT : 2;             // eights of queries whose states are joined at a time
     static constexpr int kState = kJoined * 8 * (D + 2);        // floats of a warp's state of these
-    static constexpr int kPerSm = kRowBytes == 256 || NT == 4 ? 2 : D == 128 ? (NT == 1 ? 4 : 3) : 4;
+    // Few CTAs with a deep ring each read memory faster than many with a shallow one (16 x 32768 int8 tokens of 128 dims, floor 131
+    // us: two CTAs to an SM and five stages 136, three and three 186, four and two 163; 32 x 8192 fp16 tokens of 64 dims, floor 93: two 101, three 118);
+    // rows of 64 bytes leave more to compute for each byte (32 x 8192 int8, floor 50: three 75, four 64).
+    static constexpr int kPerSm = NT == 4 || kRowBytes >= 128 ? 2 : NT == 1 ? 4 : 3;
     static constexpr int kFixed = 2 * kState * 4 + 2 * kQueryBytes + 2 * kQueries * 4 + 24 * 4 + 1024 /* alignment */ + 256 /* barriers, notes */;
     static constexpr int kStagesThatFit = ((227 * 1024 + 1024) / kPerSm - 1024 - kFixed) / (kStageBytes + kScaleBytes);
     static constexpr int kStages = kStagesThatFit < 8 ? kStagesThatFit : 8;
@@ -480,7 +484,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
             for (int m = 0; m < D / 16; ++m)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) o[n][m][j] = 0.0f;
-            top[n][0] = top[n][1] = -INFINITY;
+            top[n][0] = top[n][1] = kNone;
             sum[n][0] = sum[n][1] = 0.0f;
         }
 
@@ -517,11 +521,11 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
 
             // ---- scores: this thread's keys are key[0], key[1] ----
             const int key[2] = {S::key_of(r0), 8 + S::key_of(r0)};
-            float s[NT][4];
+            float s[NT][4], odd[NT][4];  // (even and odd steps in sums of their own: half as many products wait for one another)
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) s[n][j] = 0.0f;
+                for (int j = 0; j < 4; ++j) s[n][j] = odd[n][j] = 0.0f;
 #pragma unroll
             for (int i = 0; i < S::kChunks / 4; ++i) {
                 uint32_t w[2][4];
@@ -549,7 +553,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                     for (int n = 0; n < NT; ++n) {
                         const uint4 q = q_frag[(n * (D / 32) + (kPerChunk * i + k) / 2) * 32 + lane];
                         mma16816<S::kBf16>(s[n], rows[0], q.x, q.y);
-                        mma16816<S::kBf16>(s[n], rows[1], q.z, q.w);
+                        mma16816<S::kBf16>(odd[n], rows[1], q.z, q.w);
                     }
                 }
             }
@@ -567,13 +571,9 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     const float2 factor = *reinterpret_cast<const float2*>(q_factor + 8 * n + 2 * c);
-                    if constexpr (S::kEight) {
-                        s[n][2 * h] = fmaf(s[n][2 * h], sk * factor.x, raise);
-                        s[n][2 * h + 1] = fmaf(s[n][2 * h + 1], sk * factor.y, raise);
-                    } else {
-                        s[n][2 * h] *= factor.x;
-                        s[n][2 * h + 1] *= factor.y;
-                    }
+                    const float x = s[n][2 * h] + odd[n][2 * h], y = s[n][2 * h + 1] + odd[n][2 * h + 1];
+                    s[n][2 * h] = S::kEight ? fmaf(x, sk * factor.x, raise) : x * factor.x;
+                    s[n][2 * h + 1] = S::kEight ? fmaf(y, sk * factor.y, raise) : y * factor.y;
                 }
             }
             if (there < 16 || first_key + 15 > seen_by_all) {  // keys that are not there, or not for every query
@@ -599,30 +599,22 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                         }
                     }
             }
-            float now[NT][2];
+            // The maximum is looked for only where some exponent has left the old one behind by more than the slack.
             bool higher = false;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int x = 0; x < 2; ++x) now[n][x] = fmaxf(s[n][x], s[n][2 + x]);
-#pragma unroll
-            for (int lanes = 4; lanes < 32; lanes <<= 1)
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) now[n][x] = fmaxf(now[n][x], __shfl_xor_sync(kFullMask, now[n][x], lanes));
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int x = 0; x < 2; ++x) higher = higher || now[n][x] > top[n][x] + kSlack;
+                for (int x = 0; x < 2; ++x) higher = higher || fmaxf(s[n][x], s[n][2 + x]) > top[n][x] + kSlack;
             if (__any_sync(kFullMask, higher)) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     float shrink[2];
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        const float most = fmaxf(top[n][x], now[n][x]);
-                        shrink[x] = top[n][x] == -INFINITY ? 0.0f : exp2_of(top[n][x] - most);
+                        float most = fmaxf(top[n][x], fmaxf(s[n][x], s[n][2 + x]));
+#pragma unroll
+                        for (int lanes = 4; lanes < 32; lanes <<= 1) most = fmaxf(most, __shfl_xor_sync(kFullMask, most, lanes));
+                        shrink[x] = exp2_of(top[n][x] - most);
                         top[n][x] = most;
                         sum[n][x] *= shrink[x];
                     }
@@ -639,7 +631,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                 for (int h = 0; h < 2; ++h) {
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        const float w = exp2_of(s[n][2 * h + x] - (top[n][x] == -INFINITY ? 0.0f : top[n][x]));
+                        const float w = exp2_of(s[n][2 * h + x] - top[n][x]);
                         sum[n][x] = fmaf(w, inv[h], sum[n][x]);
                         s[n][2 * h + x] = w;
                     }
@@ -706,8 +698,8 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                     for (int x = 0; x < 2; ++x) {
                         float &mine = top[n0 + n][x], other = from[S::kJoined * kElements + 16 * n + 2 * c + x];
                         const float most = fmaxf(mine, other);
-                        keep[x] = mine == -INFINITY ? 0.0f : exp2_of(mine - most);
-                        take[x] = other == -INFINITY ? 0.0f : exp2_of(other - most);
+                        keep[x] = exp2_of(mine - most);
+                        take[x] = exp2_of(other - most);
                         sum[n0 + n][x] = sum[n0 + n][x] * keep[x] + from[S::kJoined * kElements + 16 * n + 8 + 2 * c + x] * take[x];
                         mine = most;
                     }
@@ -819,7 +811,7 @@ join_kernel(const __grid_constant__ AttnArgs a) {
     }
     pdl_wait();
     const size_t at = ((static_cast<size_t>(b) * a.rows + i) * a.n_heads + head * a.group + query - i * a.group) * D;
-    float v[kPer] = {}, top = -INFINITY, sum = 0.0f;
+    float v[kPer] = {}, top = kNone, sum = 0.0f;
     if (tiles > 0) {
         const size_t slot0 = static_cast<size_t>(unit) * a.cache.n_kv + head;
         for (int p0 = first + warp % SHARE; p0 <= last; p0 += SHARE * kBatch) {
@@ -828,7 +820,7 @@ join_kernel(const __grid_constant__ AttnArgs a) {
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
                 const int p = p0 + k * SHARE;
-                ml[k] = make_float2(-INFINITY, 0.0f);
+                ml[k] = make_float2(kNone, 0.0f);
                 if (p <= last) {
                     ml[k] = a.partial_ml[(slot0 + p) * QT + row];
                     const float* from = a.partial + ((slot0 + p) * QT + row) * D + kPer * lane;
@@ -839,7 +831,7 @@ join_kernel(const __grid_constant__ AttnArgs a) {
             float higher = top;
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) higher = fmaxf(higher, ml[k].x);
-            const float keep = top == -INFINITY ? 0.0f : exp2_of(top - higher);
+            const float keep = exp2_of(top - higher);
             sum *= keep;
 #pragma unroll
             for (int j = 0; j < kPer; ++j) v[j] *= keep;
@@ -847,7 +839,7 @@ join_kernel(const __grid_constant__ AttnArgs a) {
 #pragma unroll
             for (int k = 0; k < kBatch; ++k) {
                 if (p0 + k * SHARE > last) continue;
-                const float w = ml[k].x == -INFINITY ? 0.0f : exp2_of(ml[k].x - top);
+                const float w = exp2_of(ml[k].x - top);
                 sum = fmaf(w, ml[k].y, sum);
 #pragma unroll
                 for (int j = 0; j < kPer; ++j) v[j] = fmaf(w, part[k][j], v[j]);
@@ -863,7 +855,7 @@ join_kernel(const __grid_constant__ AttnArgs a) {
         }
         __syncthreads();
         if (warp > 0) return;
-        top = -INFINITY;
+        top = kNone;
         sum = 0.0f;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) v[j] = 0.0f;
@@ -871,7 +863,7 @@ join_kernel(const __grid_constant__ AttnArgs a) {
         for (int k = 0; k < SHARE; ++k) top = fmaxf(top, states[k][D]);
 #pragma unroll
         for (int k = 0; k < SHARE; ++k) {
-            const float w = states[k][D] == -INFINITY ? 0.0f : exp2_of(states[k][D] - top);
+            const float w = exp2_of(states[k][D] - top);
             sum = fmaf(w, states[k][D + 1], sum);
 #pragma unroll
             for (int j = 0; j < kPer; ++j) v[j] = fmaf(w, states[k][kPer * lane + j], v[j]);
