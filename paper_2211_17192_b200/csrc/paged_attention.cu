@@ -32,7 +32,7 @@ using namespace tc;
 
 constexpr int kTileKeys = 64;
 constexpr int kWarps = 4;        // that compute, with 16 of a tile's keys each
-constexpr int kMostCtas = 148 * 4;
+constexpr int kMostCtas = 148 * 5;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kSwitch = 3;       // tiles that taking up another segment costs about as much as
 constexpr float kNone = -3.0e38f;  // the running maximum where no key has been seen: finite, so that differences stay numbers
@@ -187,6 +187,22 @@ struct Shares {
 template <int QT>
 __device__ __forceinline__ int find_unit(const AttnArgs& a, int* scratch, int& unit, int& before) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    if (a.units <= 32) {  // every warp for itself
+        const int mine = lane < a.units ? unit_slots(unit_limit<QT>(a, lane)) : 0;
+        int upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int up = __shfl_up_sync(kFullMask, upto, o);
+            if (lane >= o) upto += up;
+        }
+        const int total = __shfl_sync(kFullMask, upto, 31) * a.cache.n_kv;
+        const Shares shares(total, a.grid);
+        unit = -1;
+        if (total == 0 || static_cast<int>(blockIdx.x) >= shares.ctas) return total;
+        unit = __ffs(__ballot_sync(kFullMask, shares.first(blockIdx.x) < upto * a.cache.n_kv)) - 1;
+        before = __shfl_sync(kFullMask, upto - mine, unit);
+        return total;
+    }
     const bool fits = a.units <= static_cast<int>(blockDim.x);  // (else: add up first, look then)
     int total = 0, target = 0, base = 0;
     unit = -1;
@@ -256,8 +272,9 @@ struct Shape {
     static constexpr int kState = kJoined * 8 * (D + 2);        // floats of a warp's state of these
     // Few CTAs with a deep ring each read memory faster than many with a shallow one (16 x 32768 int8 tokens of 128 dims, floor 131
     // us: two CTAs to an SM and five stages 136, three and three 186, four and two 163; 32 x 8192 fp16 tokens of 64 dims, floor 93: two 101, three 118);
-    // rows of 64 bytes leave more to compute for each byte (32 x 8192 int8, floor 50: three 75, four 64).
-    static constexpr int kPerSm = NT == 4 || kRowBytes >= 128 ? 2 : NT == 1 ? 4 : 3;
+    // rows of 64 bytes leave more to compute for each byte (32 x 8192 int8, floor 50: three 90, four 76, five 69).
+    static constexpr int kPerSm = NT == 4 || kRowBytes >= 128 ? 2 : NT == 1 ? 5 : 3;
+    static_assert(148 * kPerSm <= kMostCtas, "room for every CTA's pieces");
     static constexpr int kFixed = 2 * kState * 4 + 2 * kQueryBytes + 2 * kQueries * 4 + 24 * 4 + 1024 /* alignment */ + 256 /* barriers, notes */;
     static constexpr int kStagesThatFit = ((227 * 1024 + 1024) / kPerSm - 1024 - kFixed) / (kStageBytes + kScaleBytes);
     static constexpr int kStages = kStagesThatFit < 8 ? kStagesThatFit : 8;
@@ -521,11 +538,13 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
 
             // ---- scores: this thread's keys are key[0], key[1] ----
             const int key[2] = {S::key_of(r0), 8 + S::key_of(r0)};
-            float s[NT][4], odd[NT][4];  // (even and odd steps in sums of their own: half as many products wait for one another)
+            // (even and odd steps in sums of their own where queries are few: half as many products wait for one another)
+            constexpr bool kApart = NT < 4;
+            float s[NT][4], odd[kApart ? NT : 1][4];
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) s[n][j] = odd[n][j] = 0.0f;
+                for (int j = 0; j < 4; ++j) s[n][j] = odd[kApart ? n : 0][j] = 0.0f;
 #pragma unroll
             for (int i = 0; i < S::kChunks / 4; ++i) {
                 uint32_t w[2][4];
@@ -553,7 +572,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                     for (int n = 0; n < NT; ++n) {
                         const uint4 q = q_frag[(n * (D / 32) + (kPerChunk * i + k) / 2) * 32 + lane];
                         mma16816<S::kBf16>(s[n], rows[0], q.x, q.y);
-                        mma16816<S::kBf16>(odd[n], rows[1], q.z, q.w);
+                        mma16816<S::kBf16>(kApart ? odd[kApart ? n : 0] : s[n], rows[1], q.z, q.w);
                     }
                 }
             }
@@ -571,7 +590,11 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     const float2 factor = *reinterpret_cast<const float2*>(q_factor + 8 * n + 2 * c);
-                    const float x = s[n][2 * h] + odd[n][2 * h], y = s[n][2 * h + 1] + odd[n][2 * h + 1];
+                    float x = s[n][2 * h], y = s[n][2 * h + 1];
+                    if constexpr (kApart) {
+                        x += odd[n][2 * h];
+                        y += odd[n][2 * h + 1];
+                    }
                     s[n][2 * h] = S::kEight ? fmaf(x, sk * factor.x, raise) : x * factor.x;
                     s[n][2 * h + 1] = S::kEight ? fmaf(y, sk * factor.y, raise) : y * factor.y;
                 }
@@ -679,8 +702,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                 for (int n = 0; n < S::kJoined; ++n) {
 #pragma unroll
                     for (int m = 0; m < D / 16; ++m)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) to[n * kElements + (m * 4 + j) * 32 + lane] = o[n0 + n][m][j];
+                        reinterpret_cast<float4*>(to + n * kElements)[m * 32 + lane] = make_float4(o[n0 + n][m][0], o[n0 + n][m][1], o[n0 + n][m][2], o[n0 + n][m][3]);
                     if (r0 == 0) {
 #pragma unroll
                         for (int x = 0; x < 2; ++x) {
@@ -704,10 +726,13 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                         mine = most;
                     }
 #pragma unroll
-                    for (int m = 0; m < D / 16; ++m)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            o[n0 + n][m][j] = o[n0 + n][m][j] * keep[j & 1] + from[n * kElements + (m * 4 + j) * 32 + lane] * take[j & 1];
+                    for (int m = 0; m < D / 16; ++m) {
+                        const float4 v = reinterpret_cast<const float4*>(from + n * kElements)[m * 32 + lane];
+                        o[n0 + n][m][0] = o[n0 + n][m][0] * keep[0] + v.x * take[0];
+                        o[n0 + n][m][1] = o[n0 + n][m][1] * keep[1] + v.y * take[1];
+                        o[n0 + n][m][2] = o[n0 + n][m][2] * keep[0] + v.z * take[0];
+                        o[n0 + n][m][3] = o[n0 + n][m][3] * keep[1] + v.w * take[1];
+                    }
                 }
             };
             if (n0 > 0) compute_sync();  // (warp 0 has read the second place)
