@@ -651,7 +651,8 @@ int spec_timeout_drill(void* stream);
  *
  * A row y in 8 bits is codes c and one fp32 scale s, value c * s: with a the
  * largest |y|, s = 1 if a == 0, else a * fl(1 / 448) (e4m3) or a * fl(1 / 127) (int8), at
- * least 2^-80; c = y * (1 / s) rounded to nearest, ties to even.  A row with a NaN or
+ * least 2^-80; c = y * fl(1 / s) rounded to nearest, ties to even (spec_norm_fp8,
+ * whose y is not stored: y / s to within two roundings of 2^-24).  A row with a NaN or
  * an infinity has a scale that is not finite and reads back as NaN.
  *
  * spec_quantize_fp8: x [rows, d] fp32, bf16 or fp16 (x_dtype) to e4m3 codes

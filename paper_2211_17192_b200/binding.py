@@ -369,10 +369,12 @@ def _operand(t, name, dtypes, shape=None, contiguous=True):
 def _plain(call, first, *args):
     """Whether the module of csrc/calls.c has made the call (with all of its tensors given, and `first` among them on a GPU); one
     that it leaves is made below, where what is wrong with it is said."""
-    lib()
+    if _lib is None:
+        lib()
     if _calls is None or not getattr(first, "is_cuda", False):
         return False
-    status = getattr(_calls, call)(*args, torch._C._cuda_getDevice(), _stream())
+    device = torch._C._cuda_getDevice()
+    status = getattr(_calls, call)(*args, device, torch._C._cuda_getCurrentRawStream(device))
     if status:
         _check(status)
     return status == 0

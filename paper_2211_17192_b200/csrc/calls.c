@@ -149,11 +149,8 @@ typedef struct {
 static int look(PyObject* t, unsigned kinds, int n, long device, operand* o, int64_t* row) {
     long where;
     int fits;
-    PyObject* v = PyObject_GetAttr(t, s_is_cuda);
+    PyObject* v = PyObject_CallMethodNoArgs(t, s_get_device);  /* (-1 for one that is on no GPU) */
     if (!v) return 0;
-    Py_DECREF(v);
-    if (v != Py_True) return 0;
-    if (!(v = PyObject_CallMethodNoArgs(t, s_get_device))) return 0;
     where = PyLong_AsLong(v);
     Py_DECREF(v);
     if (where != device) return 0;

@@ -1,6 +1,8 @@
 // Rows to e4m3 codes with a scale each, as they are or behind the residual's addition and a root-mean-square norm:
 //   h = x + residual (stored in its own type; the norm is taken of what was stored)
 //   y = (h * gain) * (mean(h^2) + eps)^(-1/2),  codes and scale of y (fp8_util.cuh).
+// Codes are h * gain times 448 / max |h * gain|, which is 1 / scale with the row's factor taken out of both: two roundings instead of
+// eight, and half as many codes on the other side of a tie.
 // Bound by memory: every element is read once, held on chip across the row's one reduction (the sum of squares and the
 // largest |h * gain| travel together: the row's factor is positive, so it moves in front of the maximum, and rounding is
 // monotone), and written once.  Two kernels.  Few or narrow rows: a CTA to a row, which lies in registers, up to four groups of eight
@@ -15,6 +17,21 @@ namespace spec {
 namespace {
 
 constexpr int kWidest = 32768;  // 1024 threads of four groups of eight
+
+// The row's scale, and what its values (before the norm's factor) are multiplied with to be its codes.
+template <bool NORM>
+__device__ __forceinline__ float code_factor(uint32_t largest, float squares, int d, float eps, float& scale) {
+    float factor = 1.0f;
+    uint32_t top = largest;
+    if constexpr (NORM) {
+        factor = __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(squares, static_cast<float>(d)) + eps));
+        top = magnitude(__uint_as_float(largest) * factor);  // (a NaN among the squares makes the factor one)
+    }
+    scale = row_scale(top, kE4m3Top);
+    // a row of zeros, of values that no scale is small enough for, of no numbers, or one that is not normalised
+    if (!NORM || top == 0u || scale == kLeastScale || !(scale < 3.0e38f)) return factor * __fdiv_rn(1.0f, scale);
+    return __fdiv_rn(kE4m3Top, __uint_as_float(largest));
+}
 
 // Between its two passes a row is held as HOLD, the type it is stored in: as fp32 the registers left one CTA of a 2048 x 11008
 // call to an SM, and nothing overlapped a row's reduction (19 us).
@@ -98,12 +115,8 @@ rows_fp8_kernel(const TX* x, const TH* residual, TH* h, const float* __restrict_
         if constexpr (NORM) squares = warp_sum(lane < warps ? part_squares[lane] : 0.0f);
         largest = __reduce_max_sync(kFullMask, lane < warps ? part_largest[lane] : 0u);
     }
-    float factor = 1.0f;
-    if constexpr (NORM) {
-        factor = __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(squares, static_cast<float>(d)) + eps));
-        largest = magnitude(__uint_as_float(largest) * factor);
-    }
-    const float scale = row_scale(largest, kE4m3Top), inverse = __fdiv_rn(1.0f, scale);
+    float scale;
+    const float factor = code_factor<NORM>(largest, squares, d, eps, scale);
     if (threadIdx.x == 0) scales[row] = scale;
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
@@ -112,7 +125,7 @@ rows_fp8_kernel(const TX* x, const TH* residual, TH* h, const float* __restrict_
         if constexpr (NORM) take(gain, c0, w);
         uint32_t packed[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) packed[i] = codes_e4m3(value(g, w, 2 * i) * factor * inverse, value(g, w, 2 * i + 1) * factor * inverse);
+        for (int i = 0; i < 4; ++i) packed[i] = codes_e4m3(value(g, w, 2 * i) * factor, value(g, w, 2 * i + 1) * factor);
         if (wide) {
             if (c0 < d) *reinterpret_cast<uint2*>(codes + c0) = make_uint2(packed[0] | packed[1] << 16, packed[2] | packed[3] << 16);
         } else {
@@ -249,7 +262,6 @@ rows_fp8_stream_kernel(const __grid_constant__ RowsArgs a) {
             part_largest[turn][warp] = largest;
         }
         asm volatile("bar.sync 1, %0;" ::"n"(32 * kStreamWarps) : "memory");  // (one per row: the next row's parts lie in the other half)
-        float factor = 1.0f;
         largest = 0u;
 #pragma unroll
         for (int w = 0; w < kStreamWarps; ++w) largest = max(largest, part_largest[turn][w]);
@@ -257,11 +269,9 @@ rows_fp8_stream_kernel(const __grid_constant__ RowsArgs a) {
             squares = 0.0f;
 #pragma unroll
             for (int w = 0; w < kStreamWarps; ++w) squares += part_squares[turn][w];
-            factor = __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(squares, static_cast<float>(d)) + a.eps));
-            largest = magnitude(__uint_as_float(largest) * factor);  // (a NaN among the squares makes the factor one)
         }
-        const float scale = row_scale(largest, kE4m3Top);
-        factor *= __fdiv_rn(1.0f, scale);
+        float scale;
+        const float factor = code_factor<NORM>(largest, squares, d, a.eps, scale);
         if (threadIdx.x == 0) a.scales[row] = scale;
 #pragma unroll
         for (int g = 0; g < ITER; ++g) {

@@ -1,0 +1,171 @@
+"""A decoder block made of the 8-bit operators, as a caller with a model of its own runs it: ragged prompts into a paged cache, a
+verification pass of gamma + 1 rows, a ragged roll-back, the pass of the next iteration.  Every operator's output is checked
+against its formula in 64 bits on the inputs that it was given."""
+import numpy as np
+import pytest
+import torch
+
+import rows8
+from paper_2211_17192_b200 import binding
+from test_gpu_rows8 import NORM_REL, act64, rope_table, rotated64
+
+pytestmark = pytest.mark.gpu
+E4M3, INT8, F32, BF16, F16 = torch.float8_e4m3fn, torch.int8, torch.float32, torch.bfloat16, torch.float16
+D_MODEL, HEADS, KV_HEADS, D_HEAD, D_FF, PAGE, WIDTH = 512, 8, 2, 64, 1088, 32, 8
+
+
+class Block:
+    def __init__(self, seed, kind, batch):
+        rng = np.random.default_rng(seed)
+
+        def weight(n, k):
+            return binding.spec_quantize_fp8(torch.from_numpy(rng.standard_normal((n, k), dtype=np.float32) / np.float32(np.sqrt(k))).cuda())
+
+        qkv = (HEADS + 2 * KV_HEADS) * D_HEAD
+        self.w = {"qkv": weight(qkv, D_MODEL), "o": weight(D_MODEL, HEADS * D_HEAD), "in": weight(2 * D_FF, D_MODEL), "out": weight(D_MODEL, D_FF)}
+        self.gain = [(1 + 0.1 * torch.from_numpy(rng.standard_normal(D_MODEL, dtype=np.float32))).cuda() for _ in range(2)]
+        self.kind, self.batch = kind, batch
+        pages = batch * WIDTH + 3
+        self.pool = torch.full((pages, 2, KV_HEADS, PAGE, D_HEAD), 0x7f, dtype=torch.uint8, device="cuda").view(E4M3) if kind == E4M3 else \
+            torch.full((pages, 2, KV_HEADS, PAGE, D_HEAD), 99 if kind == INT8 else float("nan"), dtype=kind, device="cuda")
+        self.scales = torch.full(self.pool.shape[:4], float("nan"), device="cuda") if kind in rows8.TOP else None
+        self.table = rows8.make_table(rng, pages, batch, WIDTH, [WIDTH] * batch)
+        self.rope = rope_table(PAGE * WIDTH, D_HEAD).cuda()
+
+    def __call__(self, h, start, counts, check=True):
+        """h [B, rows, d] the residual stream (updated in place), start [B] positions, counts [B] rows that are no padding."""
+        batch, rows, _ = h.shape
+        flat = h.view(batch * rows, D_MODEL)
+        before = flat.clone()
+        codes, scales, _ = binding.spec_norm_fp8(flat, self.gain[0])
+        qkv = binding.spec_linear_fp8(codes, scales, *self.w["qkv"], dtype=BF16 if self.kind != F16 else F16)
+        q, k, v = (t.view(batch, rows, -1, D_HEAD) for t in qkv.view(batch, rows, -1).split([HEADS * D_HEAD, KV_HEADS * D_HEAD, KV_HEADS * D_HEAD], -1))
+        rotated = binding.spec_kv_append(k, v, self.pool, self.scales, self.table, start, counts=counts, rope=self.rope, q=q)
+        # padding rows stand behind the real ones: with the length of all rows they see more keys, and nobody reads them
+        lengths = start + rows
+        attended = binding.spec_paged_attention(rotated, self.pool, self.scales, self.table, lengths)
+        a_codes, a_scales = binding.spec_quantize_fp8(attended.view(batch * rows, -1))
+        binding.spec_linear_fp8(a_codes, a_scales, *self.w["o"], residual=flat, y=flat)
+        middle = flat.clone()
+        m_codes, m_scales, _ = binding.spec_norm_fp8(flat, self.gain[1])
+        act = binding.spec_linear_fp8(m_codes, m_scales, *self.w["in"], act="swiglu", dtype=BF16)
+        f_codes, f_scales = binding.spec_quantize_fp8(act)
+        binding.spec_linear_fp8(f_codes, f_scales, *self.w["out"], residual=flat, y=flat)
+        if check:
+            live = torch.cat([torch.arange(rows) < int(c) for c in counts])
+            self.norm(before, self.gain[0], codes, scales)
+            self.linear(codes, scales, "qkv", "none", None, qkv)
+            for b in range(batch):
+                for i in range(int(counts[b])):
+                    self.rows(q[b, i], k[b, i], v[b, i], int(start[b]) + i, b, rotated[b, i])
+            want, bound = rows8.attention64(rotated, self.pool, self.scales, self.table, lengths, D_HEAD ** -0.5)
+            err = (attended.cpu().double() - want).abs().view(batch * rows, -1)[live]
+            assert torch.all(err <= bound.view(batch * rows, -1)[live])
+            rows8.check_codes(a_codes[live.cuda()], a_scales[live.cuda()], attended.view(batch * rows, -1)[live.cuda()], E4M3)
+            self.linear(a_codes, a_scales, "o", "none", before, middle, live)
+            self.norm(middle, self.gain[1], m_codes, m_scales, live)
+            self.linear(m_codes, m_scales, "in", "swiglu", None, act, live)
+            rows8.check_codes(f_codes[live.cuda()], f_scales[live.cuda()], act[live.cuda()], E4M3)
+            self.linear(f_codes, f_scales, "out", "none", middle, flat, live)
+        return h
+
+    @staticmethod
+    def norm(x, gain, codes, scales, live=slice(None)):
+        w = x.double().cpu()
+        y = w * gain.double().cpu() / torch.sqrt((w * w).mean(-1, keepdim=True) + 1e-6)
+        rows8.check_codes(codes.cpu()[live], scales.cpu()[live], y[live], E4M3, NORM_REL)
+
+    def linear(self, codes, scales, name, act, residual, y, live=slice(None)):
+        wc, ws = self.w[name]
+        x, w = codes.float().double() * scales.double()[:, None], wc.float().double() * ws.double()[:, None]
+        z, size = x @ w.T, x.abs() @ w.abs().T
+        off = size * (2 * (x.shape[1] / 32) + 16) * 2.0 ** -23  # (as derived beside the operator's own test)
+        n = y.shape[1]
+        want = act64(z, act, n)
+        bound = off if act == "none" else (off[:, :n] * 1.13 + z[:, :n].abs() * 2.0 ** -20) * (z[:, n:].abs() + off[:, n:]) + z[:, :n].abs() * off[:, n:]
+        if residual is not None:
+            want = want + residual.double()
+            bound = bound + want.abs() * 2.0 ** -24
+        bound = bound + want.abs() * rows8.HALF_STEP[y.dtype] * 1.01 + 2.0 ** -25
+        assert torch.all(((y.double() - want).abs() <= bound).cpu()[live])
+
+    def rows(self, q, k, v, position, b, rotated):
+        page, slot = int(self.table[b, position // PAGE]), position % PAGE
+        at = torch.tensor(position)
+        want = rotated64(q.double().cpu(), at, self.rope.cpu())
+        assert torch.all((rotated.cpu().double() - want).abs() <= want.abs() * rows8.HALF_STEP[q.dtype] * 1.01 + q.abs().max().double().cpu() * 2.0 ** -21)
+        for which, x in ((0, rotated64(k.double().cpu(), at, self.rope.cpu())), (1, v.double().cpu())):
+            got = rows8.dequantised(self.pool[page, which, :, slot], None if self.scales is None else self.scales[page, which, :, slot])
+            if self.kind in rows8.TOP:
+                s = self.scales[page, which, :, slot].double().cpu()[:, None]
+                z = x / s
+                slack = x.abs().amax(-1, keepdim=True) / s * 2.0 ** -20  # (a rotation in fp32, the scale's two roundings, a reciprocal and a product)
+                assert torch.all((got / s - z).abs() <= rows8.half_step_of_code(z.abs() + slack, self.kind) + slack)
+            else:
+                assert torch.all((got - x).abs() <= x.abs() * rows8.HALF_STEP[self.kind] * 1.01 + x.abs().amax() * 2.0 ** -20)
+
+
+def stream(seed, batch, rows):
+    return torch.from_numpy(np.random.default_rng(seed).standard_normal((batch, rows, D_MODEL), dtype=np.float32)).cuda()
+
+
+def ints(*v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("kind", [E4M3, INT8, BF16, F16])
+def test_prompt_verification_rollback(kind):
+    block = Block(1, kind, 3)
+    prompts = [40, 1, 97]
+    # rows of a padded prompt beyond its count are not in the cache; the pass that needs them as keys is the next one
+    block(stream(2, 3, 97), ints(0, 0, 0), ints(*prompts), check=False)
+    lengths = ints(*prompts)
+    block(stream(3, 3, 5), lengths, ints(5, 5, 5))                     # gamma = 4
+    accepted = ints(2, 0, 4)
+    lengths = lengths + accepted + 1                                   # each sequence keeps its accepted guesses and one token more
+    second = block(stream(4, 3, 5), lengths - 1, ints(5, 5, 5))        # (that token's row is fed here)
+    # the same from a cache that never saw the rejected rows
+    fresh = Block(1, kind, 3)
+    fresh(stream(2, 3, 97), ints(0, 0, 0), ints(*prompts), check=False)
+    first = stream(3, 3, 5)
+    fresh(first, ints(*prompts), accepted, check=False)
+    again = fresh(stream(4, 3, 5), lengths - 1, ints(5, 5, 5), check=False)
+    assert torch.equal(second, again)
+    assert binding.spec_device_error() == 0
+
+
+def test_a_captured_block_is_the_same():
+    block, start, counts = Block(5, INT8, 2), ints(0, 0), ints(3, 3)
+    h = stream(6, 2, 3)
+    source = h.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        block(h, start, counts, check=False)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            h.copy_(source)
+            block(h, start, counts, check=False)
+    torch.cuda.synchronize()
+    eager = Block(5, INT8, 2)
+    for step in range(4):
+        source.copy_(stream(10 + step, 2, 3))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(h, eager(source.clone(), start, counts, check=False))
+        start += 3
+
+
+def test_calls_without_rows_do_nothing():
+    e = lambda *shape, dtype=F32: torch.empty(shape, dtype=dtype, device="cuda")
+    codes, scales = binding.spec_quantize_fp8(e(0, 64))
+    assert codes.shape == (0, 64) and scales.shape == (0,)
+    binding.spec_norm_fp8(e(0, 64), e(64), residual=e(0, 64))
+    w, ws = binding.spec_quantize_fp8(torch.ones(32, 64, device="cuda"))
+    assert binding.spec_linear_fp8(codes, scales, w, ws).shape == (0, 32)
+    pool, table = torch.zeros(2, 2, 1, 32, 64, dtype=INT8, device="cuda"), torch.zeros(2, 1, dtype=torch.int32, device="cuda")
+    s = torch.ones(2, 2, 1, 32, device="cuda")
+    binding.spec_kv_append(e(2, 0, 1, 64), e(2, 0, 1, 64), pool, s, table, ints(0, 0))
+    assert binding.spec_kv_read(pool, s, table, ints(0, 0), 0)[0].shape == (2, 0, 1, 64)
+    assert binding.spec_paged_attention(e(2, 0, 1, 64, dtype=F16), pool, s, table, ints(1, 1)).shape == (2, 0, 1, 64)
+    assert binding.spec_paged_attention(e(0, 3, 1, 64, dtype=F16), pool, s, table[:0], ints()).shape == (0, 3, 1, 64)
