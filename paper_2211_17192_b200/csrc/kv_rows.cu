@@ -4,7 +4,8 @@
 // token, so that its place is found once per thread and its angles are loaded once; a group of d_head / 16 lanes has one row of
 // one head at a time: sixteen elements to a lane, so that a pair of a rotation (j, j + d_head / 2) and the largest magnitude of the row
 // never leave the group, and nothing goes through shared memory.  (A group of twice as many lanes for every row of every token, with
-// divisions in 64 bits and the angles loaded for each row: 2 x 1024 tokens of 48 heads, append and read 21.1 us.)
+// divisions in 64 bits and the angles loaded for each row: 2 x 1024 tokens of 48 heads, append and read 21.1 us; so 14.5.)  The
+// first row's loads go out beside the chain.
 #include <algorithm>
 
 #include "paged.cuh"
@@ -12,21 +13,33 @@
 namespace spec {
 namespace {
 
-constexpr int kThreads = 128;
+constexpr int kAppendThreads = 96;  // (2 x 1024 tokens of 48 heads: 10.8 us; 64 threads 12.7, 128 12.2, 256 16.1)
+constexpr int kReadThreads = 128;   // (3.7 us; 96 threads 4.6)
 
 // Elements in the order that the rotation wants: eight at 8 l, eight at 8 l + d / 2.  grid = (tokens, shares of a token's heads).
 template <typename T, int D, int KV>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kAppendThreads)
 kv_append_kernel(const T* q, const T* k, const T* v, long long q_stride, long long k_stride, long long v_stride, int n_heads,
                  const __grid_constant__ Paged cache, void* pool, float* scales, const int32_t* start, const int32_t* counts, int rows,
                  const float2* rope, int rope_positions, T* q_out, int wide) {
     pdl_trigger();
     pdl_wait();
-    constexpr int kLanes = D / 16, kGroups = kThreads / kLanes;
+    constexpr int kLanes = D / 16, kGroups = kAppendThreads / kLanes;
     const int items = n_heads + 2 * cache.n_kv;
     const int l = threadIdx.x % kLanes;
     const size_t token = blockIdx.x;
     const int b = blockIdx.x / static_cast<unsigned>(rows), r = blockIdx.x - b * rows;
+    // (the lanes of a warp stay together, for the exchanges below: a group past the end goes along with the last item)
+    int mine = blockIdx.y * kGroups + threadIdx.x / kLanes;
+    float lo[8], hi[8];
+    const auto fetch = [&]() {
+        const int item = min(mine, items - 1), which = item < n_heads ? 0 : (item - n_heads) / cache.n_kv;
+        const T* src = item < n_heads ? q + token * q_stride + item * D
+                                      : (which == 0 ? k + token * k_stride : v + token * v_stride) + (item - n_heads - which * cache.n_kv) * D;
+        load_row(src + 8 * l, wide, lo);
+        load_row(src + 8 * l + D / 2, wide, hi);
+    };
+    fetch();  // (beside the chain that finds the token's place)
     const int first = start[b];
     if (r >= (counts ? counts[b] : rows) || first < 0 || first > 0x7fffffff - rows) return;
     const int position = first + r;
@@ -42,16 +55,11 @@ kv_append_kernel(const T* q, const T* k, const T* v, long long q_stride, long lo
             sine[i] = t.y;
         }
     }
-    // (the lanes of a warp stay together, for the exchanges below: a group past the end goes along with the last item)
-    for (int item0 = blockIdx.y * kGroups; item0 < items; item0 += gridDim.y * kGroups) {
-        const int mine = item0 + threadIdx.x / kLanes, item = min(mine, items - 1);
+    while (true) {
+        const int item = min(mine, items - 1);
         const bool live = mine < items, is_q = item < n_heads;
         const int which = is_q ? 0 : (item - n_heads) / cache.n_kv;
         const int head = is_q ? item : (item - n_heads) - which * cache.n_kv;
-        const T* src = (is_q ? q + token * q_stride : which == 0 ? k + token * k_stride : v + token * v_stride) + head * D + 8 * l;
-        float lo[8], hi[8];
-        load_row(src, wide, lo);
-        load_row(src + D / 2, wide, hi);
         if (rope && (is_q || which == 0)) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -74,7 +82,7 @@ kv_append_kernel(const T* q, const T* k, const T* v, long long q_stride, long lo
             for (int i = 0; i < 8; ++i) largest = max(largest, max(magnitude(lo[i]), magnitude(hi[i])));
 #pragma unroll
             for (int o = kLanes / 2; o > 0; o >>= 1) largest = max(largest, __shfl_xor_sync(kFullMask, largest, o));
-            if (!write) continue;
+            if (write) {
             const float scale = row_scale(largest, KV == SPEC_DTYPE_E4M3 ? kE4m3Top : kInt8Top), inverse = __fdiv_rn(1.0f, scale);
             const auto codes = [&](const float(&y)[8], int i) {
                 if constexpr (KV == SPEC_DTYPE_E4M3) return codes_e4m3(y[i] * inverse, y[i + 1] * inverse) | codes_e4m3(y[i + 2] * inverse, y[i + 3] * inverse) << 16;
@@ -84,8 +92,8 @@ kv_append_kernel(const T* q, const T* k, const T* v, long long q_stride, long lo
             out[0] = make_uint2(codes(lo, 0), codes(lo, 4));
             out[D / 16] = make_uint2(codes(hi, 0), codes(hi, 4));
             if (l == 0) scales[at] = scale;
-        } else {
-            if (!write) continue;
+            }
+        } else if (write) {
             using E = std::conditional_t<KV == SPEC_DTYPE_BF16, __nv_bfloat16, __half>;
             if constexpr (KV == SPEC_DTYPE_FP16) {  // (finite values past the type's range are held as its largest, as in the engine's caches)
 #pragma unroll
@@ -98,16 +106,19 @@ kv_append_kernel(const T* q, const T* k, const T* v, long long q_stride, long lo
             store_row(out, true, lo);
             store_row(out + D / 2, true, hi);
         }
+        mine += gridDim.y * kGroups;
+        if (mine - static_cast<int>(threadIdx.x) / kLanes >= items) break;  // (for the whole block)
+        fetch();
     }
 }
 
 template <typename T, int D, int KV>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kReadThreads)
 kv_read_kernel(const __grid_constant__ Paged cache, const void* __restrict__ pool, const float* __restrict__ scales, const int32_t* start,
                const int32_t* counts, int rows, T* k, T* v, int wide) {
     pdl_trigger();
     pdl_wait();
-    constexpr int kLanes = D / 16, kGroups = kThreads / kLanes;
+    constexpr int kLanes = D / 16, kGroups = kReadThreads / kLanes;
     const int l = threadIdx.x % kLanes;
     const size_t token = blockIdx.x;
     const int b = blockIdx.x / static_cast<unsigned>(rows), r = blockIdx.x - b * rows;
@@ -144,8 +155,8 @@ kv_read_kernel(const __grid_constant__ Paged cache, const void* __restrict__ poo
 }
 
 // A token to a CTA; its heads are shared by several where there are few tokens.
-dim3 grid_of(int tokens, int items, int lanes) {
-    const int rounds = (items * lanes + kThreads - 1) / kThreads;
+dim3 grid_of(int tokens, int items, int lanes, int threads) {
+    const int rounds = (items * lanes + threads - 1) / threads;
     return dim3(tokens, std::min(rounds, std::max(1, 1184 / tokens)));
 }
 
@@ -207,13 +218,13 @@ extern "C" int spec_kv_append(const void* q, const void* k, const void* v, int d
         return fail(SPEC_ERR_BAD_ARG, "%s: a pointer is not aligned to its elements", who);
     const int wide = aligned_to(q, 16) && aligned_to(k, 16) && aligned_to(v, 16) && aligned_to(q_out, 16) && k_stride % 8 == 0 && v_stride % 8 == 0 && (!q || q_stride % 8 == 0);
     if (static_cast<long long>(batch) * rows > 0x7fffffffll) return fail(SPEC_ERR_BAD_ARG, "%s: too many rows for one call", who);
-    const dim3 grid = grid_of(batch * rows, heads + 2 * n_kv_heads, d_head / 16);
+    const dim3 grid = grid_of(batch * rows, heads + 2 * n_kv_heads, d_head / 16, kAppendThreads);
     return with_float(dtype, [&](auto t) {
         using T = decltype(t);
         return with_kv(kv_dtype, [&](auto kv) {
             constexpr int KV = decltype(kv)::value;
             const auto go = [&](auto kernel) {
-                return launch_pdl(kernel, grid, dim3(kThreads), 0, static_cast<cudaStream_t>(stream), static_cast<const T*>(q), static_cast<const T*>(k),
+                return launch_pdl(kernel, grid, dim3(kAppendThreads), 0, static_cast<cudaStream_t>(stream), static_cast<const T*>(q), static_cast<const T*>(k),
                                   static_cast<const T*>(v), static_cast<long long>(q_stride), static_cast<long long>(k_stride), static_cast<long long>(v_stride),
                                   heads, cache, pool, scales, start, counts, rows, reinterpret_cast<const float2*>(rope), rope_positions, static_cast<T*>(q_out), wide);
             };
@@ -238,13 +249,13 @@ extern "C" int spec_kv_read(const void* pool, const float* scales, int kv_dtype,
     if (!aligned_to(k, bytes) || !aligned_to(v, bytes) || !aligned_to(start, 4) || !aligned_to(counts, 4)) return fail(SPEC_ERR_BAD_ARG, "%s: a pointer is not aligned to its elements", who);
     const int wide = aligned_to(k, 16) && aligned_to(v, 16);
     if (static_cast<long long>(batch) * rows > 0x7fffffffll) return fail(SPEC_ERR_BAD_ARG, "%s: too many rows for one call", who);
-    const dim3 grid = grid_of(batch * rows, 2 * n_kv_heads, d_head / 16);
+    const dim3 grid = grid_of(batch * rows, 2 * n_kv_heads, d_head / 16, kReadThreads);
     return with_float(dtype, [&](auto t) {
         using T = decltype(t);
         return with_kv(kv_dtype, [&](auto kv) {
             constexpr int KV = decltype(kv)::value;
             const auto go = [&](auto kernel) {
-                return launch_pdl(kernel, grid, dim3(kThreads), 0, static_cast<cudaStream_t>(stream), cache, pool, scales, start, counts, rows,
+                return launch_pdl(kernel, grid, dim3(kReadThreads), 0, static_cast<cudaStream_t>(stream), cache, pool, scales, start, counts, rows,
                                   static_cast<T*>(k), static_cast<T*>(v), wide);
             };
             return d_head == 64 ? go(kv_read_kernel<T, 64, KV>) : go(kv_read_kernel<T, 128, KV>);
