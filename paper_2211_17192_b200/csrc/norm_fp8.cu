@@ -174,7 +174,6 @@ rows_fp8_stream_kernel(const __grid_constant__ RowsArgs a) {
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
-    pdl_trigger();
     pdl_wait();
     const int d = a.d, x_bytes = d * static_cast<int>(sizeof(TX));
     const bool summed = NORM && a.residual;
@@ -198,6 +197,7 @@ rows_fp8_stream_kernel(const __grid_constant__ RowsArgs a) {
             __syncwarp();
             if (++stage == a.stages) { stage = 0; ++use; }
         }
+        pdl_trigger();  // (behind the last row that is asked for: let in at the top, the next kernel's CTAs come to lie unevenly; 2048 x 4096 13.9 us, 12.2 so)
         if (limit != kSpinLimit) {  // nothing may still be on its way when the CTA leaves
             for (int s = 0; s < a.stages; ++s) {
                 mbar_wait(&full_bar[s], 0, 1 << 14);
