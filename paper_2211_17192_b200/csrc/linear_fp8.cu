@@ -117,21 +117,23 @@ __device__ __forceinline__ LaneColumn lane_column(const LinearArgs& a, int tile,
 __device__ __forceinline__ float gate(float x, float s) { return __fdividef(x, 1.0f + __expf(-s)); }
 __device__ __forceinline__ float gelu_argument(float x) { return x * fmaf(0.0713548162726f * x, x, 1.5957691216057f); }
 
-// COLS neighbouring accumulator columns (rows r0 .. of x, `count` of them) of a warp's 32 rows of W to y.  Everything is loaded
-// before anything is stored: the loads are in flight together (one column after the other took 0.2 to 0.4 us each).
+// The residual of COLS neighbouring accumulator columns (rows r0 .. of x, `count` of them) of a warp's 32 rows of W.
 template <typename T, int COLS>
-__device__ __forceinline__ void finish(const LinearArgs& a, const LaneColumn& c, int r0, int count, float (&z)[COLS]) {
-    float x_scale[COLS], add[COLS];
-    const float* scales = a.x_scales + r0;
-    const size_t at = static_cast<size_t>(r0) * a.n_out + (c.column < 0 ? 0 : c.column);
-    const T* residual = static_cast<const T*>(a.residual) + at;
-    T* y = static_cast<T*>(a.y) + at;
+__device__ __forceinline__ void load_residual(const LinearArgs& a, const LaneColumn& c, int r0, int count, T (&add)[COLS]) {
+    if (!a.residual) return;
+    const T* from = static_cast<const T*>(a.residual) + static_cast<size_t>(r0) * a.n_out + (c.column < 0 ? 0 : c.column);
+#pragma unroll
+    for (int i = 0; i < COLS; ++i) add[i] = i < count && c.column >= 0 ? from[static_cast<size_t>(i) * a.n_out] : from_float<T>(0.0f);
+}
+// These columns to y.  Everything is loaded before anything is stored: the loads are in flight together (one column after the
+// other took 0.2 to 0.4 us each).
+template <typename T, int COLS>
+__device__ __forceinline__ void finish(const LinearArgs& a, const LaneColumn& c, const float* scales /* of these rows of x */, int r0, int count,
+                                       float (&z)[COLS], const T (&add)[COLS]) {
+    float x_scale[COLS];
+    T* y = static_cast<T*>(a.y) + static_cast<size_t>(r0) * a.n_out + (c.column < 0 ? 0 : c.column);
 #pragma unroll
     for (int i = 0; i < COLS; ++i) x_scale[i] = i < count ? scales[i] : 0.0f;
-    if (a.residual) {
-#pragma unroll
-        for (int i = 0; i < COLS; ++i) add[i] = i < count && c.column >= 0 ? to_float(residual[static_cast<size_t>(i) * a.n_out]) : 0.0f;
-    }
 #pragma unroll
     for (int i = 0; i < COLS; ++i) z[i] = fmaf(z[i] * x_scale[i], c.scale, c.bias);
     if (a.act == kActGelu) {
@@ -152,7 +154,7 @@ __device__ __forceinline__ void finish(const LinearArgs& a, const LaneColumn& c,
     if (c.column < 0) return;
     if (a.residual) {
 #pragma unroll
-        for (int i = 0; i < COLS; ++i) z[i] += add[i];
+        for (int i = 0; i < COLS; ++i) z[i] += to_float(add[i]);
     }
 #pragma unroll
     for (int i = 0; i < COLS; ++i)
@@ -262,9 +264,11 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
         if (reader && ok)
             for (int c0 = 0; c0 < valid; c0 += 16) {
                 float z[16];
+                T add[16];
+                load_residual<T, 16>(a, column, row0 + c0, valid - c0, add);
                 tmem_ld16(acc + c0, reinterpret_cast<uint32_t(&)[16]>(z));
                 tmem_ld_wait();
-                finish<T, 16>(a, column, row0 + c0, valid - c0, z);
+                finish<T, 16>(a, column, a.x_scales + row0 + c0, row0 + c0, valid - c0, z, add);
             }
     } else {
         // CTA r finishes columns [r each, (r + 1) each): the others' sums of these lie in its exchange as [CTA][four columns][128][4]
@@ -292,6 +296,8 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
             const int c1 = min(valid, static_cast<int>(rank + 1) * each);
             for (int c0 = rank * each; c0 < c1; c0 += 8) {
                 float z[8];
+                T add[8];
+                load_residual<T, 8>(a, column, row0 + c0, c1 - c0, add);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) z[i] = 0.0f;
                 for (uint32_t p = 0; p < splits; ++p) {
@@ -306,7 +312,7 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
                         z[i + 3] += v.w;
                     }
                 }
-                finish<T, 8>(a, column, row0 + c0, c1 - c0, z);
+                finish<T, 8>(a, column, a.x_scales + row0 + c0, row0 + c0, c1 - c0, z, add);
             }
         }
     }
@@ -334,7 +340,9 @@ int codes_map(const void* base, int planes, int rows, int k, int box_planes, int
 // the ring, a warp of the even CTA issues the MMAs, eight warps drain the accumulators, of which there are two: the next tile is
 // multiplied while the last is finished and written.
 constexpr int kEpilogueWarps = 8;
+constexpr int kWideRows = 256;  // most rows of x per tile
 constexpr int kWideThreads = 32 * (2 + kEpilogueWarps);
+
 
 __device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {
     uint32_t r;
@@ -381,6 +389,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kWideThreads, 1)
 linear_fp8_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ LinearArgs a) {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    __shared__ float row_scales[kEpilogueWarps][kWideRows / 2];
     const int half = a.tokens / 2, stage_bytes = kTileBytes + half * kBlockK;
     uint64_t* full_bar = reinterpret_cast<uint64_t*>(smem + a.stages * stage_bytes);  // (the even CTA's count both CTAs' bytes)
     uint64_t* empty_bar = full_bar + kMaxStages;
@@ -472,18 +481,35 @@ linear_fp8_wide_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_c
         }
     } else {
         const int quarter = warp & 3, first_col = ((warp - 2) >> 2) * 16;
+        float* scales = row_scales[warp - 2];
         int buf = 0, turn = 0;
         for (int tile = pair; tile < a.tiles; tile += pairs) {
             const LaneColumn column = lane_column(a, (tile / a.token_tiles) * 2 + static_cast<int>(rank), quarter, lane);
             const int row0 = (tile % a.token_tiles) * a.tokens, valid = min(a.tokens, a.rows - row0);
+            // The loads of the epilogue wait behind the ring's: the scales of the warp's rows are fetched once per tile, while it is
+            // multiplied, and the residual sixteen columns ahead (2048 x 11008 x 4096 with an fp32 residual 79 -> 71 us, 2048 x 4096 x 4096
+            // 46 -> 41; two or three times sixteen ahead: no better).
+            __syncwarp();
+#pragma unroll
+            for (int i = lane; i < kWideRows / 2; i += 32) {
+                const int r = first_col + i / 16 * 32 + i % 16;
+                scales[i] = r < valid ? a.x_scales[row0 + r] : 0.0f;
+            }
+            __syncwarp();
+            T coming[16];
+            load_residual<T, 16>(a, column, row0 + first_col, valid - first_col, coming);
             if (!mbar_wait_warp(&acc_full[buf], turn & 1, a.limit)) { ok = false; break; }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t acc = tmem + buf * 256 + (static_cast<uint32_t>(quarter * 32) << 16);
             for (int c0 = first_col; c0 < valid; c0 += 32) {
                 float z[16];
+                T add[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) add[i] = coming[i];
+                load_residual<T, 16>(a, column, row0 + c0 + 32, valid - c0 - 32, coming);
                 tmem_ld16(acc + c0, reinterpret_cast<uint32_t(&)[16]>(z));
                 tmem_ld_wait();
-                finish<T, 16>(a, column, row0 + c0, valid - c0, z);
+                finish<T, 16>(a, column, scales + (c0 - first_col) / 2, row0 + c0, valid - c0, z, add);
             }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
@@ -540,12 +566,13 @@ int launch_wide(const void* x, const void* w, int k, LinearArgs a, cudaStream_t 
     constexpr int kPairs = 74;  // one CTA per SM
     const int per_tile = gated ? kTileM : 2 * kTileM, w_tiles = (a.n_out + per_tile - 1) / per_tile;
     a.k_blocks = (k + kBlockK - 1) / kBlockK;
-    // Rows of x per tile: as many as make the busiest pair's tiles the shortest (a tile costs its columns and about as much again as
-    // 16 for its start).
+    // Rows of x per tile: as many as make the busiest pair's tiles the shortest, where a tile costs its rows and 60 more (a k-block brings
+    // 128 rows of W to a CTA however few rows of x meet them).  4096 x 22016 gated: 224 rows in two tiles of 112, three rounds, 27.8 us, in
+    // one, two rounds, 31.7; 256 rows in two of 128, three rounds, 28.6, in four of 64, five rounds, 37.6, in one, two rounds, 34.5.
     long long best = 0;
     for (int tokens = 256; tokens >= 64; tokens -= 16) {
         const int token_tiles = (a.rows + tokens - 1) / tokens;
-        const long long rounds = (static_cast<long long>(w_tiles) * token_tiles + kPairs - 1) / kPairs, cost = rounds * (tokens + 16);
+        const long long rounds = (static_cast<long long>(w_tiles) * token_tiles + kPairs - 1) / kPairs, cost = rounds * (tokens + 60);
         if (best == 0 || cost < best) {
             best = cost;
             a.tokens = tokens;
@@ -554,13 +581,13 @@ int launch_wide(const void* x, const void* w, int k, LinearArgs a, cudaStream_t 
     }
     a.tiles = w_tiles * a.token_tiles;
     const int stage_bytes = kTileBytes + a.tokens / 2 * kBlockK;
-    a.stages = std::min(kMaxStages, (227 * 1024 - 1024 - 512) / stage_bytes);
+    a.stages = std::min(kMaxStages, (227 * 1024 - 1024 - 512 - kEpilogueWarps * kWideRows * 2) / stage_bytes);
     CUtensorMap mw, mx;
     int status = codes_map(w, gated ? 2 : 1, a.n_out, k, gated ? 2 : 1, gated ? 16 : kTileM, &mw);
     if (status == SPEC_OK) status = codes_map(x, 1, a.rows, k, 0, a.tokens / 2, &mx);
     if (status != SPEC_OK) return status;
     static std::atomic<unsigned long long> configured{0};
-    status = allow_shared_memory(configured, linear_fp8_wide_kernel<T>, 227 * 1024);
+    status = allow_shared_memory(configured, linear_fp8_wide_kernel<T>, 227 * 1024 - kEpilogueWarps * kWideRows * 2);
     if (status != SPEC_OK) return status;
     return launch_pdl(linear_fp8_wide_kernel<T>, dim3(2 * std::min(kPairs, a.tiles)), dim3(kWideThreads), a.stages * stage_bytes + 1024 + 512, stream, mw, mx, a);
 }

@@ -1,6 +1,10 @@
 """A decoder block made of the 8-bit operators, as a caller with a model of its own runs it: ragged prompts into a paged cache, a
 verification pass of gamma + 1 rows, a ragged roll-back, the pass of the next iteration.  Every operator's output is checked
 against its formula in 64 bits on the inputs that it was given."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -169,3 +173,45 @@ def test_calls_without_rows_do_nothing():
     assert binding.spec_kv_read(pool, s, table, ints(0, 0), 0)[0].shape == (2, 0, 1, 64)
     assert binding.spec_paged_attention(e(2, 0, 1, 64, dtype=F16), pool, s, table, ints(1, 1)).shape == (2, 0, 1, 64)
     assert binding.spec_paged_attention(e(0, 3, 1, 64, dtype=F16), pool, s, table[:0], ints()).shape == (0, 3, 1, 64)
+
+
+FIRST = """
+import torch
+from paper_2211_17192_b200 import binding
+B = torch.bfloat16
+x, gain = torch.randn(300, 2048, device="cuda").to(B), torch.ones(2048, device="cuda")
+w = torch.randn(512, 2048, device="cuda").to(torch.float8_e4m3fn)
+codes, scales = torch.empty(300, 2048, dtype=torch.float8_e4m3fn, device="cuda"), torch.ones(300, device="cuda")
+ws, y, few = torch.ones(512, device="cuda"), torch.empty(300, 512, device="cuda"), torch.empty(3, 512, device="cuda")
+pool = torch.zeros(4, 2, 2, 32, 128, dtype=torch.int8, device="cuda")
+ps, table, start = torch.ones(4, 2, 2, 32, device="cuda"), torch.arange(4, dtype=torch.int32, device="cuda").view(1, 4), torch.zeros(1, dtype=torch.int32, device="cuda")
+k, out = torch.randn(1, 100, 2, 128, device="cuda").to(B), torch.empty(1, 5, 8, 128, dtype=B, device="cuda")
+q, lengths = torch.randn(1, 5, 8, 128, device="cuda").to(B), torch.full((1,), 100, dtype=torch.int32, device="cuda")
+ko, vo = torch.empty(1, 100, 2, 128, device="cuda"), torch.empty(1, 100, 2, 128, device="cuda")
+work = torch.empty(binding.spec_paged_attention_workspace_bytes(1, 5, 8, 2, 128), dtype=torch.uint8, device="cuda")
+def step():
+    binding.spec_norm_fp8(x, gain, codes=codes, scales=scales)
+    binding.spec_quantize_fp8(x[:2], codes=codes[:2], scales=scales[:2])
+    binding.spec_linear_fp8(codes, scales, w, ws, y=y)
+    binding.spec_linear_fp8(codes[:3], scales[:3], w, ws, y=few)
+    binding.spec_kv_append(k, k, pool, ps, table, start)
+    binding.spec_kv_read(pool, ps, table, start, 100, k=ko, v=vo)
+    binding.spec_paged_attention(q, pool, ps, table, lengths, out=out, workspace=work)
+side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+torch.cuda.synchronize()
+with torch.cuda.graph(graph, stream=side):
+    step()
+graph.replay()
+torch.cuda.synchronize()
+got = [t.clone() for t in (codes.float(), scales, y, few, ko, out)]
+step()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(got, (codes.float(), scales, y, few, ko, out))) and torch.isfinite(out.float()).all()
+print("captured first")
+"""
+
+
+def test_a_first_call_may_be_a_captured_one():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", FIRST], cwd=root, capture_output=True, text=True, timeout=180)
+    assert done.returncode == 0 and "captured first" in done.stdout, done.stderr[-2000:]
