@@ -366,15 +366,16 @@ def _operand(t, name, dtypes, shape=None, contiguous=True):
     return t.data_ptr()
 
 
-def _plain(call, first, *args):
-    """Whether the module of csrc/calls.c has made the call (with all of its tensors given, and `first` among them on a GPU); one
-    that it leaves is made below, where what is wrong with it is said."""
-    if _lib is None:
-        lib()
-    if _calls is None or not getattr(first, "is_cuda", False):
-        return False
-    device = torch._C._cuda_getDevice()
-    status = getattr(_calls, call)(*args, device, torch._C._cuda_getCurrentRawStream(device))
+# The module of csrc/calls.c makes a call whose tensors are all given; one that it leaves is made in the function itself, where what is
+# wrong with it is said.
+_device, _raw_stream = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else None, getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _short(first):
+    return _calls is not None and getattr(first, "is_cuda", False)
+
+
+def _made(status):
     if status:
         _check(status)
     return status == 0
@@ -412,8 +413,10 @@ def _pool_args(pool, scales, page_table, batch):
 def spec_quantize_fp8(x, codes=None, scales=None):
     """Rows in e4m3 with a scale each: x [rows, d] fp32, bf16 or fp16 CUDA -> (codes [rows, d] float8_e4m3fn, scales [rows] fp32),
     value = code * scale.  Also how the weights of `spec_linear_fp8` are made."""
-    if codes is not None and scales is not None and _plain("quantize", x, x, codes, scales):
-        return codes, scales
+    if codes is not None and scales is not None and _short(x):
+        device = _device()
+        if _made(_calls.quantize(x, codes, scales, device, _raw_stream(device))):
+            return codes, scales
     _need(isinstance(x, torch.Tensor) and x.dim() == 2, "x must be [rows, d]")
     where = _operand(x, "x", _FLOATS)
     rows, d = x.shape
@@ -429,8 +432,10 @@ def spec_norm_fp8(x, gain, eps=1e-6, residual=None, h=None, codes=None, scales=N
     rmsnorm(h) * gain; x [rows, d] fp32, bf16 or fp16, gain [d] fp32, residual and h [rows, d] fp32 or of x's type.
     Returns (codes, scales, h); h is allocated when a residual is given without it, may be the residual itself, and is
     None when neither is given."""
-    if codes is not None and scales is not None and _plain("norm", x, x, gain, eps, residual, h, codes, scales):
-        return codes, scales, h
+    if codes is not None and scales is not None and _short(x):
+        device = _device()
+        if _made(_calls.norm(x, gain, eps, residual, h, codes, scales, device, _raw_stream(device))):
+            return codes, scales, h
     _need(isinstance(x, torch.Tensor) and x.dim() == 2, "x must be [rows, d]")
     where = _operand(x, "x", _FLOATS)
     rows, d = x.shape
@@ -454,9 +459,12 @@ def spec_linear_fp8(x, x_scales, w, w_scales, bias=None, act="none", residual=No
     x_scales [rows] and w_scales [n_w]; act "none", "gelu", "silu" (n_out = n_w), "gated_gelu" or "swiglu" (n_out = n_w / 2, gate
     rows first); bias [n_w] fp32; residual and y [rows, n_out] of one type, y is allocated in the residual's type or `dtype`
     when not given and may be the residual."""
-    _need(act in ACTIVATIONS, f"act must be one of {', '.join(ACTIVATIONS)}")
-    if y is not None and _plain("linear", x, x, x_scales, w, w_scales, bias, ACTIVATIONS[act], residual, y):
-        return y
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {', '.join(ACTIVATIONS)}")
+    if y is not None and _short(x):
+        device = _device()
+        if _made(_calls.linear(x, x_scales, w, w_scales, bias, ACTIVATIONS[act], residual, y, device, _raw_stream(device))):
+            return y
     _need(isinstance(x, torch.Tensor) and x.dim() == 2 and isinstance(w, torch.Tensor) and w.dim() == 2 and x.shape[1] == w.shape[1],
           "x must be [rows, k] and w [n_w, k]")
     (rows, k), n_w = x.shape, w.shape[0]
@@ -480,8 +488,10 @@ def spec_kv_append(k, v, pool, scales, page_table, start, counts=None, rope=None
     bf16 or fp16, parts of one projection's output or tensors of their own; pool [pages, 2, kv heads, page size, d_head];
     scales [pages, 2, kv heads, page size] fp32 for 8-bit pools, else None; page_table [B, max_pages], start [B],
     counts [B] int32.  Row i of sequence b goes to position start[b] + i if i < counts[b].  Returns q_out (None without q)."""
-    if (q is None or q_out is not None) and _plain("append", k, k, v, pool, scales, page_table, start, counts, rope, q, q_out):
-        return q_out
+    if (q is None or q_out is not None) and _short(k):
+        device = _device()
+        if _made(_calls.append(k, v, pool, scales, page_table, start, counts, rope, q, q_out, device, _raw_stream(device))):
+            return q_out
     _need(isinstance(k, torch.Tensor) and k.dim() == 4, "k must be [B, rows, heads, d_head]")
     batch, rows, n_kv, d = k.shape
     where, at, kv_dtype, pages, page_size, table, width, pool_heads, pool_d = _pool_args(pool, scales, page_table, batch)
@@ -510,8 +520,10 @@ def spec_kv_read(pool, scales, page_table, start, rows, counts=None, dtype=torch
     """The cached rows at start[b] .. start[b] + counts[b] - 1 (`rows` of them without counts) of every sequence, widened:
     (k, v) [B, rows, kv heads, d_head] of `dtype`, zeros where there is no row, or into the tensors given, whose other rows
     stay as they are."""
-    if k is not None and v is not None and _plain("read", pool, pool, scales, page_table, start, rows, counts, k, v):
-        return k, v
+    if k is not None and v is not None and _short(pool):
+        device = _device()
+        if _made(_calls.read(pool, scales, page_table, start, rows, counts, k, v, device, _raw_stream(device))):
+            return k, v
     _need(isinstance(page_table, torch.Tensor) and page_table.dim() == 2, "page_table must be [B, max_pages]")
     batch = page_table.shape[0]
     where, at, kv_dtype, pages, page_size, table, width, n_kv, d = _pool_args(pool, scales, page_table, batch)
@@ -533,9 +545,11 @@ def spec_paged_attention(q, pool, scales, page_table, lengths, scale=None, out=N
     bf16 or fp16, the cache as in `spec_kv_append`, lengths [B] int32 the tokens cached with the new ones; row i sees the keys at
     and before position lengths[b] - rows + i.  scale defaults to d_head ** -0.5.  Returns out, of q's shape and type; it and
     the workspace are allocated when not given."""
-    if out is not None and workspace is not None and \
-            _plain("attention", q, q, pool, scales, page_table, lengths, q.shape[-1] ** -0.5 if scale is None else scale, out, workspace):
-        return out
+    if out is not None and workspace is not None and _short(q):
+        device = _device()
+        if _made(_calls.attention(q, pool, scales, page_table, lengths, q.shape[-1] ** -0.5 if scale is None else scale, out, workspace, device,
+                                  _raw_stream(device))):
+            return out
     _need(isinstance(q, torch.Tensor) and q.dim() == 4, "q must be [B, rows, heads, d_head]")
     batch, rows, heads, d = q.shape
     where, at, kv_dtype, pages, page_size, table, width, n_kv, pool_d = _pool_args(pool, scales, page_table, batch)

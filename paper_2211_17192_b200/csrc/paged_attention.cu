@@ -313,7 +313,7 @@ struct Run {
         if (++head == a.cache.n_kv) {
             head = 0;
             do {
-                ++unit;
+                if (++unit >= a.units) return false;
                 open(a);
             } while (limit == 0);
         }
