@@ -682,7 +682,8 @@ int spec_timeout_drill(void* stream);
  * types scales [pages][K, V][n_kv_heads][page_size] fp32 (a scale per token and
  * head; those of rows that are read have to be above zero).  page_size: a power
  * of two from 32 to 256; d_head 64 or 128.  page_table [batch][max_pages] int32:
- * the page of each page_size positions of a sequence.  An entry outside [0, pages)
+ * the page of each page_size positions of a sequence, below 2^31 - 256 positions;
+ * batch <= 65535, n_kv_heads <= 1024.  An entry outside [0, pages)
  * is not followed: rows there are neither written nor read back, and attention
  * goes on as if the keys there did not exist.  Pages may be shared for reading;
  * two rows written to one place in one call, or by calls that may overlap, race.
@@ -690,17 +691,18 @@ int spec_timeout_drill(void* stream);
  * spec_kv_append: row i of sequence b (k, v [batch, rows, n_kv_heads, d_head] of
  *   `dtype`, one row k_stride / v_stride ELEMENTS behind the last, heads dense)
  *   goes to position start[b] + i, for i < counts[b] (counts NULL: all rows);
- *   rows beyond, negative starts and positions past the table are left out.  rope
- *   (may be NULL) [rope_positions][d_head / 2][2] fp32, (cos, sin) of position *
- *   frequency j, rotates K's pairs (j, j + d_head / 2) first: x cos - y sin,
- *   y cos + x sin; positions past the table are left out.  q (may be NULL,
+ *   rows beyond and negative starts are left out; a position past the page table has
+ *   no page.  rope (may be NULL) [rope_positions][d_head / 2][2] fp32, (cos, sin) of
+ *   position * frequency j, rotates K's pairs (j, j + d_head / 2) first:
+ *   x cos - y sin, y cos + x sin; positions past this table are left out.  q (may be NULL,
  *   with q_out) [batch, rows, n_heads, d_head] of `dtype` with q_stride gets the
  *   same rotation, rounded into q_out (dense; may be q if that is dense); rows
- *   that are left out are not touched.  fp16 pools hold +-65504 for what is beyond.
+ *   that are left out are not touched, those whose position has no page are
+ *   rotated.  fp16 pools hold +-65504 for what is beyond.
  *
- * spec_kv_read: the rows that an append with the same start, counts and rows has
- *   written, into k and v [batch, rows, n_kv_heads, d_head] of `dtype`; rows that
- *   are left out are not touched.
+ * spec_kv_read: what lies where an append with the same start, counts and rows (and
+ *   no rope) writes, into k and v [batch, rows, n_kv_heads, d_head] of `dtype`; rows
+ *   that are left out or have no page are not touched.
  *
  * spec_paged_attention: lengths [batch] counts the cached tokens of a sequence
  *   with the `rows` new ones; row i stands at position p = lengths[b] - rows + i
@@ -715,6 +717,9 @@ int spec_timeout_drill(void* stream);
  *   pools: as they are), weights are rounded to 16 bits for the second product,
  *   all sums are fp32.  workspace: spec_paged_attention_workspace_bytes() bytes,
  *   256-byte aligned, contents arbitrary, not shared by calls that may overlap.
+ *   Scales of an 8-bit pool are 16-byte aligned here.  rows <= 65536, heads of a KV
+ *   head <= 1024, rows times these <= 2^20; batch * n_kv_heads * (blocks of 32
+ *   queries) * (tiles of 64 keys that the table has room for, and three) <= 2^30.
  *
  * Errors: SPEC_ERR_BAD_ARG for null pointers, sizes, types, alignments or strides
  * other than described (nothing is launched then); SPEC_ERR_CUDA if a launch fails.

@@ -113,8 +113,8 @@ static PyObject* sample(PyObject* self, PyObject* const* a, Py_ssize_t count) {
 }
 
 /* ---- the 8-bit operators ----
- * A call with all its outputs given, as a serving loop makes it: norm of one row of 768 22.7 -> 6.9 us call after call, append and read
- * of 32 x 7 rows 71.7 -> 16, attention with its workspace 31.4 -> 14 (the checks in Python are a microsecond or two per tensor). */
+ * A call with all its outputs given, as a serving loop makes it: norm of one row of 768 22.7 -> 5.7 us call after call, append and read
+ * of 32 x 7 rows 71.7 -> 12.2, attention with its workspace 31.4 -> 8.9 (the checks in Python are a microsecond or two per tensor). */
 typedef int (*quantize_fn)(const void*, int, int, int, void*, float*, void*);
 typedef int (*norm_fn)(const void*, int, const void*, void*, int, const float*, float, int, int, void*, float*, void*);
 typedef int (*linear_fn)(const void*, const float*, const void*, const float*, const float*, int, const void*, void*, int, int, int, int, void*);
@@ -174,7 +174,7 @@ static int look(PyObject* t, unsigned kinds, int n, long device, operand* o, int
         for (int i = 0; fits && i < 4; ++i) s[i] = PyLong_AsSsize_t(PyTuple_GET_ITEM(v, i));
         Py_DECREF(v);
         if (!fits || PyErr_Occurred() || s[3] != 1 || s[2] != o->dims[3]) return 0;
-        *row = o->dims[1] > 1 ? s[1] : s[0];
+        *row = o->dims[1] > 1 ? s[1] : o->dims[0] > 1 ? s[0] : o->dims[2] * o->dims[3];  /* (a lone row's own stride may be anything) */
         if (o->dims[0] > 1 && o->dims[1] > 1 && s[0] != o->dims[1] * s[1]) return 0;
     } else {
         if (!(v = PyObject_CallMethodNoArgs(t, s_is_contiguous))) return 0;

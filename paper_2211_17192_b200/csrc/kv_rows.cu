@@ -114,7 +114,7 @@ kv_append_kernel(const T* q, const T* k, const T* v, long long q_stride, long lo
 
 template <typename T, int D, int KV>
 __global__ void __launch_bounds__(kReadThreads)
-kv_read_kernel(const __grid_constant__ Paged cache, const void* __restrict__ pool, const float* __restrict__ scales, const int32_t* start,
+kv_read_kernel(const __grid_constant__ Paged cache, const void* pool, const float* scales, const int32_t* start,
                const int32_t* counts, int rows, T* k, T* v, int wide) {
     pdl_trigger();
     pdl_wait();
@@ -184,7 +184,7 @@ int check_paged(const char* who, const void* pool, const float* scales, int kv_d
     if (!eight && kv_dtype != SPEC_DTYPE_FP16 && kv_dtype != SPEC_DTYPE_BF16) return fail(SPEC_ERR_BAD_ARG, "%s: kv_dtype %d", who, kv_dtype);
     if (d_head != 64 && d_head != 128) return fail(SPEC_ERR_BAD_ARG, "%s: d_head=%d (64 or 128)", who, d_head);
     if (page_size < 32 || page_size > 256 || (page_size & (page_size - 1))) return fail(SPEC_ERR_BAD_ARG, "%s: page_size=%d (a power of two in 32..256)", who, page_size);
-    if (n_kv_heads < 1 || n_kv_heads > 1024 || pages < 1 || max_pages < 1 || max_pages > 0x7fffffff / page_size || batch < 0 || batch > 65535)
+    if (n_kv_heads < 1 || n_kv_heads > 1024 || pages < 1 || max_pages < 1 || max_pages > 0x7fffff00 / page_size || batch < 0 || batch > 65535)
         return fail(SPEC_ERR_BAD_ARG, "%s: n_kv_heads=%d pages=%d max_pages=%d batch=%d", who, n_kv_heads, pages, max_pages, batch);
     if (!pool || !page_table || (eight && !scales)) return fail(SPEC_ERR_BAD_ARG, "%s: null pointer", who);
     if (!aligned_to(pool, 16) || !aligned_to(page_table, 4) || !aligned_to(scales, 4)) return fail(SPEC_ERR_BAD_ARG, "%s: a pointer is not aligned (the pool to 16 bytes)", who);

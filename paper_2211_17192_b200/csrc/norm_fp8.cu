@@ -41,6 +41,7 @@ rows_fp8_kernel(const TX* x, const TH* residual, TH* h, const float* __restrict_
                 float* __restrict__ scales) {
     pdl_trigger();
     pdl_wait();
+    gain = after_wait(gain);
     const size_t row = blockIdx.x;
     x += row * d;
     codes += row * d;

@@ -826,15 +826,16 @@ join_kernel(const __grid_constant__ AttnArgs a) {
         total *= a.cache.n_kv;
         front = front * a.cache.n_kv + head * (tiles + kSwitch) + kSwitch;
     }
-    if (row >= QT || i >= a.rows) return;
     int first = 0, last = 0;
     if (tiles > 0) {
         const Shares shares(total, a.grid);
         first = shares.owner(front);
         last = shares.owner(front + tiles - 1);
-        if (first == last) return;  // (written by the CTA that has all of it)
     }
+    // (Every CTA waits, also one with nothing to do: the kernel behind waits for this one alone, which must not end ahead of the one in front.)
     pdl_wait();
+    if (row >= QT || i >= a.rows) return;
+    if (tiles > 0 && first == last) return;  // (written by the CTA that has all of it)
     const size_t at = ((static_cast<size_t>(b) * a.rows + i) * a.n_heads + head * a.group + query - i * a.group) * D;
     float v[kPer] = {}, top = kNone, sum = 0.0f;
     if (tiles > 0) {

@@ -160,6 +160,65 @@ def test_a_captured_block_is_the_same():
         start += 3
 
 
+@pytest.mark.parametrize("batch,rows,length", [(1, 3, 40), (9, 7, 64), (64, 64, 64), (3, 5, 65)])
+def test_what_follows_attention_waits_for_it(batch, rows, length):
+    # contexts of one tile: no CTA has anything to join, and the kernel behind attention reads what it wrote all the same
+    rng = np.random.default_rng(batch)
+    pool, scales = rows8.make_cache(rng, batch * 2, 2, 64, 128, INT8)
+    table = rows8.make_table(rng, batch * 2, batch, 2, [2] * batch)
+    lengths = torch.full((batch,), length, dtype=torch.int32, device="cuda")
+    qs = [torch.from_numpy(rng.standard_normal((batch, rows, 8, 128), dtype=np.float32)).to(BF16).cuda() for _ in range(2)]
+    out = torch.zeros_like(qs[0])
+    work = torch.empty(binding.spec_paged_attention_workspace_bytes(batch, rows, 8, 2, 128), dtype=torch.uint8, device="cuda")
+    want = []
+    for q in qs:
+        binding.spec_paged_attention(q, pool, scales, table, lengths, out=out, workspace=work)
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in binding.spec_quantize_fp8(out.view(batch * rows, -1))])
+        torch.cuda.synchronize()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    taken = [[torch.empty_like(t) for t in want[0]] for _ in range(8)]
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        for i, (c, s) in enumerate(taken):
+            binding.spec_paged_attention(qs[i % 2], pool, scales, table, lengths, out=out, workspace=work)
+            binding.spec_quantize_fp8(out.view(batch * rows, -1), codes=c, scales=s)
+    for _ in range(5):
+        graph.replay()
+        torch.cuda.synchronize()
+        for i, (c, s) in enumerate(taken):
+            assert torch.equal(c.view(torch.uint8), want[i % 2][0].view(torch.uint8)) and torch.equal(s, want[i % 2][1])
+
+
+def test_a_lone_row_whose_stride_means_nothing():
+    # [heads, 1, d] turned round: one row, whose stride torch gives as d
+    q, k = (torch.randn(n, 1, 64, device="cuda").to(BF16).transpose(0, 1)[None] for n in (4, 2))
+    assert k.stride(0) < 2 * 64
+    results = []
+    for x, y in ((q, k), (q.clone(memory_format=torch.contiguous_format), k.clone(memory_format=torch.contiguous_format))):
+        pool, table, start = torch.zeros(2, 2, 2, 32, 64, dtype=BF16, device="cuda"), torch.zeros(1, 2, dtype=torch.int32, device="cuda"), ints(5)
+        turned = binding.spec_kv_append(y, y, pool, None, table, start, rope=rope_table(64, 64).cuda(), q=x, q_out=torch.empty(1, 1, 4, 64, dtype=BF16, device="cuda"))
+        work = torch.empty(binding.spec_paged_attention_workspace_bytes(1, 1, 4, 2, 64), dtype=torch.uint8, device="cuda")
+        out = binding.spec_paged_attention(x, pool, None, table, start + 1, out=torch.empty(1, 1, 4, 64, dtype=BF16, device="cuda"), workspace=work)
+        results.append((pool, turned, out))
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
+def test_a_position_past_the_page_table_has_no_page():
+    # K and V are left out, q is turned as everywhere
+    rope = rope_table(80, 64)
+    k, q = torch.randn(1, 4, 1, 64, device="cuda"), torch.randn(1, 4, 2, 64, device="cuda")
+    pool = torch.zeros(2, 2, 1, 32, 64, dtype=F16, device="cuda")
+    out = binding.spec_kv_append(k, k, pool, None, ints(1)[None], ints(30), rope=rope.cuda(), q=q)
+    want = rotated64(q[0].cpu().double(), torch.arange(30, 34), rope)
+    assert torch.all((out[0].cpu().double() - want).abs() <= 2.0 ** -21 * (q[0].cpu().double().abs() + q[0].cpu().double().abs().roll(32, -1)))
+    assert pool[1, :, :, 30:].all() and not pool[1, :, :, :30].any() and not pool[0].any()
+    # (positions 32 and 33: zeros come back)
+    k_out, _ = binding.spec_kv_read(pool, None, ints(1)[None], ints(30), 4)
+    assert k_out[0, :2].all() and not k_out[0, 2:].any()
+
+
 def test_calls_without_rows_do_nothing():
     e = lambda *shape, dtype=F32: torch.empty(shape, dtype=dtype, device="cuda")
     codes, scales = binding.spec_quantize_fp8(e(0, 64))
