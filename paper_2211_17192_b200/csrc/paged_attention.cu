@@ -14,7 +14,8 @@
 // else.  A segment that several CTAs share leaves (maximum, sum, weighted rows) per CTA in the workspace, and a second
 // kernel joins them in order.  No atomics: the same bits every time.
 //
-// A CTA has four warps, each with 16 of a tile's 64 keys and all queries of the block, 8, 16 or 32.  The keys take the M side of both
+// More than 32 queries to a KV head: paged_attention_wide.cuh.  Up to there a CTA has four warps, each with 16 of a tile's 64 keys and all
+// queries of the block, 8, 16 or 32.  The keys take the M side of both
 // products (scores [key][query], weighted rows [dim][query]): queries come in eights then, and a K or V fragment is widened once
 // for all of them.  (Queries on the M side, sixteen at least: twice the multiplications and registers for a lone token of four
 // heads.)  One more warp asks for the tiles of the whole run, segment after segment, by TMA (halves of 32 keys, which never straddle a
@@ -32,7 +33,8 @@ using namespace tc;
 
 constexpr int kTileKeys = 64;
 constexpr int kWarps = 4;        // that compute, with 16 of a tile's keys each
-constexpr int kMostCtas = 148 * 5;
+// CTAs of a launch whose blocks have so many queries, at most.
+constexpr int most_ctas(int queries) { return 148 * (queries == 8 ? 5 : queries == 16 ? 3 : 2); }
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kSwitch = 3;       // tiles that taking up another segment costs about as much as
 constexpr float kNone = -3.0e38f;  // the running maximum where no key has been seen: finite, so that differences stay numbers
@@ -47,12 +49,13 @@ struct AttnArgs {
     const void* q;
     void* out;
     const int32_t* lengths;
-    float* partial;    // [slots][queries of a block][D]
-    float2* partial_ml;  // [slots][queries of a block]: maximum, sum
+    // Of each CTA two places: for the segment that began before its run, and for the one that goes on behind it.
+    float* partial;      // [CTA][2][queries of a block][D]
+    float2* partial_ml;  // [CTA][2][queries of a block]: maximum, sum
     long long q_stride;
     float scale;
     int batch, rows, n_heads, group, blocks, units;  // blocks: of queries per (sequence, KV head); units = batch * blocks
-    int q_bf16, grid;
+    int q_bf16, q_wide /* q's rows start on 16 bytes */, grid;
     uint32_t by_group;  // ceil(2^32 / group) for groups of two and more
     // The token of a query of a (sequence, KV head); exact, since query * group stays below 2^31.
     __device__ __forceinline__ int token_of(int query) const { return group == 1 ? query : static_cast<int>(__umulhi(static_cast<uint32_t>(query), by_group)); }
@@ -274,7 +277,7 @@ struct Shape {
     // us: two CTAs to an SM and five stages 136, three and three 186, four and two 163; 32 x 8192 fp16 tokens of 64 dims, floor 93: two 101, three 118);
     // rows of 64 bytes leave more to compute for each byte (32 x 8192 int8, floor 50: three 90, four 76, five 69).
     static constexpr int kPerSm = NT == 4 || kRowBytes >= 128 ? 2 : NT == 1 ? 5 : 3;
-    static_assert(148 * kPerSm <= kMostCtas, "room for every CTA's pieces");
+    static_assert(148 * kPerSm <= most_ctas(kQueries), "room for every CTA's pieces");
     static constexpr int kFixed = 2 * kState * 4 + 2 * kQueryBytes + 2 * kQueries * 4 + 24 * 4 + 1024 /* alignment */ + 256 /* barriers, notes */;
     static constexpr int kStagesThatFit = ((227 * 1024 + 1024) / kPerSm - 1024 - kFixed) / (kStageBytes + kScaleBytes);
     static constexpr int kStages = kStagesThatFit < 8 ? kStagesThatFit : 8;
@@ -745,7 +748,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
         }
         if (warp == 0) {
             const bool whole = run.tile0 == 0 && run.tile1 == run.tiles;
-            const size_t slot = static_cast<size_t>(blockIdx.x) + static_cast<size_t>(run.unit) * a.cache.n_kv + run.head;
+            const size_t slot = 2 * static_cast<size_t>(blockIdx.x) + (run.tile0 == 0 ? 1 : 0);
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -786,6 +789,8 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
     }
     if (limit != kSpinLimit && lane == 0) atomicCAS(&g_paged_error, 0, 2);
 }
+
+#include "paged_attention_wide.cuh"
 
 // Joins the states of a segment that several CTAs had, in their order; a segment without a key gets its zeros here.  SHARE warps of
 // a CTA have one query: they take its pieces in turn, eight at a time with all their loads in flight.  Where segments are few, and
@@ -839,7 +844,6 @@ join_kernel(const __grid_constant__ AttnArgs a) {
     const size_t at = ((static_cast<size_t>(b) * a.rows + i) * a.n_heads + head * a.group + query - i * a.group) * D;
     float v[kPer] = {}, top = kNone, sum = 0.0f;
     if (tiles > 0) {
-        const size_t slot0 = static_cast<size_t>(unit) * a.cache.n_kv + head;
         for (int p0 = first + warp % SHARE; p0 <= last; p0 += SHARE * kBatch) {
             float2 ml[kBatch];
             float part[kBatch][kPer];
@@ -848,8 +852,9 @@ join_kernel(const __grid_constant__ AttnArgs a) {
                 const int p = p0 + k * SHARE;
                 ml[k] = make_float2(kNone, 0.0f);
                 if (p <= last) {
-                    ml[k] = a.partial_ml[(slot0 + p) * QT + row];
-                    const float* from = a.partial + ((slot0 + p) * QT + row) * D + kPer * lane;
+                    const size_t slot = 2 * static_cast<size_t>(p) + (p == first ? 1 : 0);
+                    ml[k] = a.partial_ml[slot * QT + row];
+                    const float* from = a.partial + (slot * QT + row) * D + kPer * lane;
 #pragma unroll
                     for (int j = 0; j < kPer; ++j) part[k][j] = from[j];
                 }
@@ -903,10 +908,12 @@ join_kernel(const __grid_constant__ AttnArgs a) {
     }
 }
 
-// Queries of a block, in eights: as many as those of a (sequence, KV head) fill, at most four.
-int query_eights(int rows, int group) {
+// Queries of a block: those of a (sequence, KV head) in eights, two or four of them, and from 33 on the wide kernel's 128.  (32 sequences,
+// 8 KV heads of 128 dims: 28 queries over 2048 int8 tokens 61 us so, 75 wide; 72 queries of 12 heads, 48 sequences of 300 int8 tokens, 124
+// in blocks of 32, 66 wide; two prompts of 1024 rows, 4096 queries a head, 202 and 105, over bf16 rows 231 and 88.)
+int queries_of_block(int rows, int group) {
     const int queries = rows * group;
-    return queries <= 8 ? 1 : queries <= 16 ? 2 : 4;
+    return queries <= 8 ? 8 : queries <= 16 ? 16 : queries <= 32 ? 32 : 128;
 }
 
 size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
@@ -922,37 +929,49 @@ int rows_map(const AttnArgs& a, bool eight, int d, int box_bytes, CUtensorMap* o
                       box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, out);
 }
 
-template <int D, int KV, int NT>
-int launch(const AttnArgs& args, cudaStream_t stream) {
-    using S = Shape<D, KV, NT>;
-    static std::atomic<unsigned long long> configured{0};
-    int status = once_on_this_device(configured, []() -> int {
-        const auto kernel = paged_attention_kernel<D, KV, NT>;
-        SPEC_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));
-        if (S::kShift) {  // (a thread that takes registers waits until its block has them: never, were the launch's too few)
-            cudaFuncAttributes f;
-            SPEC_CUDA_TRY(cudaFuncGetAttributes(&f, kernel));
-            if (f.numRegs * S::kThreads < 32 * kWarps * (S::kTaken + S::kLeft)) return fail(SPEC_ERR_CUDA, "spec_paged_attention: built with %d registers a thread", f.numRegs);
-        }
+// The kernel over the tiles, whose blocks have QT queries, and the one that joins what it leaves.
+template <int D, int QT, typename Kernel>
+int launch(Kernel kernel, int per_sm, int threads, int registers, int smem, bool eight, int box_bytes, const AttnArgs& args, cudaStream_t stream, std::atomic<unsigned long long>& configured) {
+    int status = once_on_this_device(configured, [&]() -> int {
+        SPEC_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        cudaFuncAttributes f;  // (a thread that takes registers waits until its block has them: never, were the launch's too few)
+        SPEC_CUDA_TRY(cudaFuncGetAttributes(&f, kernel));
+        if (f.numRegs < registers) return fail(SPEC_ERR_CUDA, "spec_paged_attention: built with %d registers a thread", f.numRegs);
         return SPEC_OK;
     });
     if (status != SPEC_OK) return status;
     AttnArgs a = args;
-    a.grid = 148 * S::kPerSm;
+    a.grid = 148 * per_sm;
     CUtensorMap map;
-    status = rows_map(a, S::kEight, D, S::kBoxBytes, &map);
+    status = rows_map(a, eight, D, box_bytes, &map);
     if (status != SPEC_OK) return status;
-    status = launch_pdl(paged_attention_kernel<D, KV, NT>, dim3(a.grid), dim3(S::kThreads), S::kSmem, stream, map, a);
+    status = launch_pdl(kernel, dim3(a.grid), dim3(threads), smem, stream, map, a);
     if (status != SPEC_OK) return status;
-    const int segments = a.units * a.cache.n_kv, queries = static_cast<int>(std::min<long long>(S::kQueries, static_cast<long long>(a.rows) * a.group));
-    if (segments * 4 <= a.grid) return launch_pdl(join_kernel<D, S::kQueries, 4>, dim3(segments, queries), dim3(128), 0, stream, a);
-    return launch_pdl(join_kernel<D, S::kQueries, 1>, dim3(segments, (queries + 3) / 4), dim3(128), 0, stream, a);
+    const int segments = a.units * a.cache.n_kv, queries = static_cast<int>(std::min<long long>(QT, static_cast<long long>(a.rows) * a.group));
+    if (segments * 4 <= a.grid) return launch_pdl(join_kernel<D, QT, 4>, dim3(segments, queries), dim3(128), 0, stream, a);
+    return launch_pdl(join_kernel<D, QT, 1>, dim3(segments, (queries + 3) / 4), dim3(128), 0, stream, a);
+}
+template <int D, int KV, int NT>
+int launch_narrow(const AttnArgs& a, cudaStream_t stream) {
+    using S = Shape<D, KV, NT>;
+    static std::atomic<unsigned long long> configured{0};
+    return launch<D, S::kQueries>(paged_attention_kernel<D, KV, NT>, S::kPerSm, S::kThreads, S::kShift ? (S::kTaken + S::kLeft) / 2 : 0, S::kSmem, S::kEight, S::kBoxBytes, a, stream, configured);
+}
+template <int D, int KV>
+int launch_wide(const AttnArgs& a, cudaStream_t stream) {
+    using S = Wide<D, KV>;
+    static std::atomic<unsigned long long> configured{0};
+    return launch<D, S::kQueries>(paged_attention_wide_kernel<D, KV>, S::kPerSm, S::kThreads, S::kLaunched, S::kSmem, S::kEight, S::kBoxBytes, a, stream, configured);
 }
 
 template <int D, int KV>
 int launch_tiles(const AttnArgs& a, cudaStream_t stream) {
-    const int eights = query_eights(a.rows, a.group);
-    return eights == 1 ? launch<D, KV, 1>(a, stream) : eights == 2 ? launch<D, KV, 2>(a, stream) : launch<D, KV, 4>(a, stream);
+    switch (queries_of_block(a.rows, a.group)) {
+        case 8: return launch_narrow<D, KV, 1>(a, stream);
+        case 16: return launch_narrow<D, KV, 2>(a, stream);
+        case 32: return launch_narrow<D, KV, 4>(a, stream);
+        default: return launch_wide<D, KV>(a, stream);
+    }
 }
 
 template <int D>
@@ -972,6 +991,9 @@ bool fits(int batch, int rows, int n_heads, int n_kv_heads, int d_head) {
 }
 long long units_of(int batch, int rows, int group, int queries) { return static_cast<long long>(batch) * ((static_cast<long long>(rows) * group + queries - 1) / queries); }
 
+// Places for what two and more CTAs share of a segment: two for each.
+size_t slots_for(int queries) { return 2 * static_cast<size_t>(most_ctas(queries)); }
+
 }  // namespace
 
 int paged_attention_take_error() {
@@ -986,8 +1008,7 @@ int paged_attention_take_error() {
 extern "C" size_t spec_paged_attention_workspace_bytes(int batch, int rows, int n_heads, int n_kv_heads, int d_head) {
     using namespace spec;
     if (!fits(batch, rows, n_heads, n_kv_heads, d_head)) return 0;
-    const int group = n_heads / n_kv_heads, queries = 8 * query_eights(rows, group);
-    const size_t slots = kMostCtas + static_cast<size_t>(units_of(batch, rows, group, queries)) * n_kv_heads;
+    const size_t queries = queries_of_block(rows, n_heads / n_kv_heads), slots = slots_for(static_cast<int>(queries));
     return align256(slots * queries * d_head * 4) + align256(slots * queries * 8);
 }
 
@@ -1011,14 +1032,14 @@ extern "C" int spec_paged_attention(const void* q, int dtype, int64_t q_stride, 
     if (scales && !aligned_to(scales, 16)) return fail(SPEC_ERR_BAD_ARG, "%s: scales have to start on 16 bytes", who);
     if (static_cast<long long>(pages) * 2 * n_kv_heads > 0x7fffffffll) return fail(SPEC_ERR_BAD_ARG, "%s: pages=%d", who, pages);
     a.group = n_heads / n_kv_heads;
-    const int queries = 8 * query_eights(rows, a.group);
+    const int queries = queries_of_block(rows, a.group);
     const long long units = units_of(batch, rows, a.group, queries);
     // (slots are counted in 32 bits, with room for a CTA's share on top)
     const long long slots_each = (static_cast<long long>(max_pages) * page_size + kTileKeys - 1) / kTileKeys + kSwitch;
     if (units * n_kv_heads > (1ll << 30) / slots_each) return fail(SPEC_ERR_BAD_ARG, "%s: too many rows for one call", who);
     if (!workspace || workspace_bytes < spec_paged_attention_workspace_bytes(batch, rows, n_heads, n_kv_heads, d_head) || !aligned_to(workspace, 256))
         return fail(SPEC_ERR_BAD_ARG, "%s: workspace missing, too small or not 256-byte aligned", who);
-    const size_t slots = kMostCtas + static_cast<size_t>(units) * n_kv_heads;
+    const size_t slots = slots_for(queries);
     a.pool = pool;
     a.scales = scales;
     a.q = q;
@@ -1034,6 +1055,7 @@ extern "C" int spec_paged_attention(const void* q, int dtype, int64_t q_stride, 
     a.units = static_cast<int>(units);
     a.blocks = a.units / batch;
     a.q_bf16 = dtype == SPEC_DTYPE_BF16;
+    a.q_wide = aligned_to(q, 16) && q_stride % 8 == 0;
     a.by_group = a.group > 1 ? static_cast<uint32_t>((0xffffffffull + a.group) / a.group) : 0u;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return d_head == 64 ? launch_kv<64>(a, kv_dtype, st) : launch_kv<128>(a, kv_dtype, st);
