@@ -135,3 +135,45 @@ def test_captured_calls_follow_their_inputs():
         torch.cuda.synchronize()
         for q, out in zip(qs, outs):
             assert torch.equal(out, binding.spec_paged_attention(q, pool, scales, table, at))
+
+
+@pytest.mark.parametrize("kind,dtype", [(INT8, BF16), (F16, F16)])
+@pytest.mark.parametrize("rows", [2, 12])
+def test_pages_past_32_bits_of_the_pool(kind, dtype, rows):
+    rng = np.random.default_rng(6)
+    heads, size, d = 2, 256, 128
+    pages = 2 ** 32 // (2 * heads * size * d) + 5  # elements: past 2^32
+    small, small_scales = rows8.make_cache(rng, 6, heads, size, d, kind)
+    pool = torch.zeros(pages, 2, heads, size, d, dtype=kind, device="cuda")
+    scales = torch.ones(pool.shape[:4], device="cuda") if kind in rows8.TOP else None
+    pool.view(torch.uint8)[pages - 6:] = small.view(torch.uint8)
+    if scales is not None:
+        scales[pages - 6:] = small_scales
+    table = rows8.make_table(rng, 6, 2, 3, [3, 2])
+    q = torch.from_numpy(rng.standard_normal((2, rows, 8, d), dtype=np.float32)).to(dtype).cuda()
+    at = torch.tensor([700, 300], dtype=torch.int32, device="cuda")
+    far = torch.where(table >= 0, table + pages - 6, table)
+    assert torch.equal(binding.spec_paged_attention(q, pool, scales, far, at), binding.spec_paged_attention(q, small, small_scales, table, at))
+
+
+def test_calls_on_two_streams_at_once():
+    # attention and a linear layer, both with tensor memory of an SM, beside each other
+    rng = np.random.default_rng(7)
+    pool, scales = rows8.make_cache(rng, 120, 2, 32, 128, E4M3)
+    table = rows8.make_table(rng, 120, 4, 30, [30] * 4)
+    q = torch.from_numpy(rng.standard_normal((4, 100, 16, 128), dtype=np.float32)).to(BF16).cuda()
+    at = torch.tensor([960, 100, 333, 901], dtype=torch.int32, device="cuda")
+    x, w = (binding.spec_quantize_fp8(torch.from_numpy(rng.standard_normal((n, 1024), dtype=np.float32)).cuda()) for n in (200, 2000))
+    want = [binding.spec_paged_attention(q, pool, scales, table, at), binding.spec_linear_fp8(*x, *w), binding.spec_linear_fp8(x[0][:5], x[1][:5], *w)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    got = [[] for _ in streams]
+    for _ in range(20):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[i].append(binding.spec_paged_attention(q, pool, scales, table, at) if i == 0 else
+                              binding.spec_linear_fp8(*x, *w) if i == 1 else binding.spec_linear_fp8(x[0][:5], x[1][:5], *w))
+    torch.cuda.synchronize()
+    for results, expected in zip(got, want):
+        for result in results:
+            assert torch.equal(result, expected)
