@@ -505,6 +505,10 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap map, const __gri
                     tmem_st_wait();
                     tmem_before_sync();
                 }
+                // A wait tells a phase from its neighbours only.  S of this tile says that the second product before the last has ended, and the
+                // waits behind the segment (here for its O, of the issuer for the next S) are for the second product of this tile: the one between
+                // them has to have ended first, or they pass a product early where a warp is a tile behind the others.
+                if (t + 1 == run.tile1 && t > run.tile0) wait(o_done, g - 1);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&p_full[g & 1]);
             }

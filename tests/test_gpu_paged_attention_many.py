@@ -177,3 +177,39 @@ def test_calls_on_two_streams_at_once():
     for results, expected in zip(got, want):
         for result in results:
             assert torch.equal(result, expected)
+
+
+@pytest.mark.parametrize("kind,dtype", KINDS)
+@pytest.mark.parametrize("slow", [0, 3])
+def test_a_warp_that_is_behind_the_others(kind, dtype, slow):
+    # 32 neighbouring queries (a warp's) meet a higher score in every tile, so that all they have added up is scaled down each time; the
+    # others' largest is in the first tile.  Segments of two tiles and more, many to a CTA: each one's end and the next one's start.
+    rng = np.random.default_rng(8)
+    batch, heads, d, size, rows = 40, 8, 128, 64, 128
+    lengths = [128 + 64 * (b % 5) for b in range(batch)]
+    used = [-(-l // size) for l in lengths]
+    x = torch.from_numpy(rng.standard_normal((sum(used), 2, heads, size, d), dtype=np.float32))
+    table = rows8.make_table(rng, sum(used), batch, max(used), used)
+    x[:, 0, :, :, 0] = 0
+    for b in range(batch):
+        for j in range(used[b]):
+            x[int(table[b, j]), 0, :, :, 0] = 4.0 * j
+    scales = None
+    if kind in rows8.TOP:
+        scales = rows8.scale64(x.double(), kind).float()
+        z = x * (1.0 / scales)[..., None]
+        x = z.clamp(-448, 448) if kind == E4M3 else z.round()
+        scales = scales.cuda()
+    pool = x.to(kind).cuda()
+    q = torch.from_numpy(rng.standard_normal((batch, rows, heads, d), dtype=np.float32)) * 0.1
+    q[..., 0] = -8.0
+    q[:, 32 * slow:32 * slow + 32, :, 0] = 8.0
+    q = q.to(dtype).cuda()
+    at = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    got = binding.spec_paged_attention(q, pool, scales, table, at, scale=1.0)
+    some = torch.tensor([0, 1, 2, 18, 39])
+    want, bound = rows8.attention64(q[some], pool, scales, table[some.cuda()], at[some.cuda()], 1.0)
+    assert torch.all((got[some].cpu().double() - want).abs() <= bound)
+    for _ in range(20):
+        assert torch.equal(binding.spec_paged_attention(q, pool, scales, table, at, scale=1.0), got)
+    assert binding.spec_device_error() == 0
