@@ -717,7 +717,9 @@ int spec_timeout_drill(void* stream);
  *   pools: as they are), weights are rounded to 16 bits for the second product,
  *   all sums are fp32.  workspace: spec_paged_attention_workspace_bytes() bytes,
  *   256-byte aligned, contents arbitrary, not shared by calls that may overlap.
- *   Scales of an 8-bit pool are 16-byte aligned here.  rows <= 65536, heads of a KV
+ *   Scales of an 8-bit pool are 16-byte aligned here.  Weights are rounded against the
+ *   largest weight times V scale of a row; a V row of zeros with the scale 1, as it is
+ *   appended, does not count there.  rows <= 65536, heads of a KV
  *   head <= 1024, rows times these <= 2^20; batch * n_kv_heads * (blocks of 32
  *   queries) * (tiles of 64 keys that the table has room for, and three) <= 2^30.
  *

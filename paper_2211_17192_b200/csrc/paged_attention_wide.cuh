@@ -278,10 +278,16 @@ paged_attention_wide_kernel(const __grid_constant__ CUtensorMap map, const __gri
                     if (which == 0 && tid < 4) edges[4 * (g & 1) + tid] = tid == 0 ? note : 0;
                     if constexpr (S::kEight) {
                         if (tid < kTileKeys) {
-                            const float s = raw_scales[stage * kTileKeys + tid];
+                            float s = raw_scales[stage * kTileKeys + tid];
                             if (which == 0) {
                                 tile_info[tid] = there(tid) ? s : 0.0f;
                             } else {
+                                if (s == 1.0f) {  // (seldom)
+                                    uint32_t some = 0u;
+#pragma unroll 1
+                                    for (int x = 0; x < S::kRowBytes / 16; ++x) some |= some_code<KV>(*reinterpret_cast<const uint4*>(from + Shape<D, KV, 1>::place(tid, x)));
+                                    if (some == 0u) s = kScaleOfZeros;
+                                }
                                 const bool number = magnitude(s) < 0x7f800000u;
                                 tile_info[kTileKeys + tid] = number ? log2_of(s) : NAN;
                                 tile_info[2 * kTileKeys + tid] = there(tid) && number ? reciprocal_of(s) : 0.0f;
