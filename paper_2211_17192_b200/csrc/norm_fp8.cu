@@ -18,6 +18,12 @@ namespace {
 
 constexpr int kWidest = 32768;  // 1024 threads of four groups of eight
 
+// max(m, |v|), a NaN if v or m is one (as bits NaNs are the largest too: both kernels give a row that has one the same scale).
+__device__ __forceinline__ float larger_magnitude(float m, float v) {
+    asm("{\n\t.reg .f32 a;\n\tabs.f32 a, %1;\n\tmax.NaN.f32 %0, %0, a;\n\t}" : "+f"(m) : "f"(v));
+    return m;
+}
+
 // The row's scale, and what its values (before the norm's factor) are multiplied with to be its codes.
 template <bool NORM>
 __device__ __forceinline__ float code_factor(uint32_t largest, float squares, int d, float eps, float& scale) {
@@ -243,7 +249,7 @@ rows_fp8_stream_kernel(const __grid_constant__ RowsArgs a) {
                 for (int i = 0; i < 8; ++i) {
                     squares += v[g][i] * v[g][i];
                     v[g][i] *= kGains ? gains[kGains ? g : 0][i] : w[i];
-                    most = fmaxf(most, fabsf(v[g][i]));  // (passes over a NaN, which the squares have)
+                    most = larger_magnitude(most, v[g][i]);
                 }
             } else {
 #pragma unroll

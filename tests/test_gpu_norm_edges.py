@@ -1,0 +1,87 @@
+"""Norm and quantisation of rows that hold no numbers, or numbers at the ends of the range, in calls of few rows and of many: the same rows
+get the same answers."""
+import numpy as np
+import pytest
+import torch
+
+import rows8
+from paper_2211_17192_b200 import binding
+from test_gpu_rows8 import NORM_REL, normal
+
+pytestmark = pytest.mark.gpu
+E4M3, F32, BF16, F16 = torch.float8_e4m3fn, torch.float32, torch.bfloat16, torch.float16
+WIDTHS = [2048, 4096, 8192, 16384]  # (a kernel of its own each in calls of many rows)
+
+
+def same(a, b):
+    return torch.equal(a.float().nan_to_num(12345.0), b.float().nan_to_num(12345.0))
+
+
+@pytest.mark.parametrize("d", WIDTHS)
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_quantize_rows_at_the_ends(d, dtype):
+    if d == 16384 and dtype == F32:
+        d = 14336  # (56 KB, the longest row that many rows of this type take the same way)
+    x = normal(d, 300, d)
+    if dtype != F16:
+        x[1] *= 1e30
+        x[2] *= 1e-30
+        x[6, 3] = 3e38
+    x[3] = 0
+    x[4, d - 1] = float("nan")
+    x[5, d // 2] = -float("inf")
+    x[7] = float("nan")
+    x[299, 0] = float("inf")
+    x = x.to(dtype).cuda()
+    codes, scales = binding.spec_quantize_fp8(x)
+    none = [4, 5, 7, 299]
+    fine = [r for r in range(300) if r not in none]
+    rows8.check_codes(codes[fine], scales[fine], x[fine], E4M3)
+    assert not torch.isfinite(scales[none]).any() and torch.isnan(codes[none].float() * scales[none, None]).all()
+    for rows in (list(range(8)), none):
+        few = binding.spec_quantize_fp8(x[rows].contiguous())
+        assert same(few[0], codes[rows]) and same(few[1], scales[rows])
+
+
+@pytest.mark.parametrize("d", WIDTHS)
+@pytest.mark.parametrize("dtype,h_dtype", [(F32, F32), (BF16, BF16), (BF16, F32), (F16, F16)])
+@pytest.mark.parametrize("summed", [True, False])
+def test_norm_rows_that_are_no_numbers(d, dtype, h_dtype, summed):
+    rows = 160
+    if (dtype, d, summed) == (F32, 16384, True):
+        d = 6144  # (48 KB a row with its residual)
+    x, residual, gain = normal(d, rows, d).to(dtype), normal(d + 1, rows, d).to(h_dtype) if summed else None, 1 + 0.1 * normal(d + 2, d)
+    x[1, 3] = float("nan")
+    x[2, d - 1] = float("inf")
+    x[3] = 0
+    if summed:
+        residual[3] = 0
+        residual[4, 5] = -float("inf")
+        none = [1, 2, 4]
+    else:
+        none = [1, 2]
+    gain[3] = 0.0  # (takes the NaN out of the products, not out of the row)
+    gain[d - 1] = 0.0
+    args = lambda r: (x[r].contiguous().cuda(), gain.cuda(), 1e-6, None if residual is None else residual[r].contiguous().cuda())
+    codes, scales, _ = binding.spec_norm_fp8(*args(slice(None)))
+    assert torch.isnan(codes[none].float() * scales[none, None]).all() and not torch.isfinite(scales[none]).any()
+    fine = [r for r in range(rows) if r not in none]
+    w = x.float() + (residual.float() if summed else 0)
+    w = (w.to(h_dtype) if summed else w).double()
+    y = w * gain.double() / torch.sqrt((w * w).mean(-1, keepdim=True) + 1e-6)
+    rows8.check_codes(codes[fine], scales[fine], y[fine], E4M3, NORM_REL)
+    few = binding.spec_norm_fp8(*args(slice(0, 6)))
+    assert torch.equal(torch.isnan(few[1]), torch.isnan(scales[:6])) and torch.equal(torch.isnan(few[0].float()), torch.isnan(codes[:6].float()))
+
+
+@pytest.mark.parametrize("d", WIDTHS)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_a_gain_that_is_no_number_is_in_every_row(d, dtype, value):
+    x, gain = normal(d, 160, d).to(dtype).cuda(), torch.ones(d, device="cuda")
+    gain[5] = value
+    x[7, 5] = 0  # (0 * inf)
+    x[8] = 0
+    for part in (x, x[:9].contiguous()):
+        codes, scales, _ = binding.spec_norm_fp8(part, gain)
+        assert not torch.isfinite(scales).any() and torch.isnan(codes.float() * scales[:, None]).all()
