@@ -663,7 +663,9 @@ int spec_timeout_drill(void* stream);
  *   stored; y = (h * gain) * (mean(h^2) + eps)^(-1/2) over the row; codes and
  *   scales of y.  residual [rows, d] and h [rows, d] have type h_dtype; residual
  *   NULL: h = x; h NULL: the sum is not stored (and not rounded).  h may be
- *   residual, or x where the types are the same.  gain [d] fp32, eps > 0.
+ *   residual, or x where the types are the same.  gain [d] fp32, eps > 0.  A row
+ *   whose squares add up past fp32's range (2^128) reads back as NaN, as one does
+ *   whose y holds a NaN or an infinity.
  *
  * spec_linear_fp8: x [rows, k] and w [n_w, k] e4m3 codes with x_scales [rows] and
  *   w_scales [n_w], k a multiple of 16, codes 16-byte aligned:

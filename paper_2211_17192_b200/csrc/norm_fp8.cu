@@ -30,8 +30,9 @@ __device__ __forceinline__ float code_factor(uint32_t largest, float squares, in
     float factor = 1.0f;
     uint32_t top = largest;
     if constexpr (NORM) {
-        factor = __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(squares, static_cast<float>(d)) + eps));
-        top = magnitude(__uint_as_float(largest) * factor);  // (a NaN among the squares makes the factor one)
+        // (squares that add up past fp32's range are no mean: a factor of zero would make a row of zeros of the largest there are)
+        factor = squares < INFINITY ? __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(squares, static_cast<float>(d)) + eps)) : NAN;
+        top = magnitude(__uint_as_float(largest) * factor);
     }
     scale = row_scale(top, kE4m3Top);
     // a row of zeros, of values that no scale is small enough for, of no numbers, or one that is not normalised

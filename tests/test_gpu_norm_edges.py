@@ -85,3 +85,22 @@ def test_a_gain_that_is_no_number_is_in_every_row(d, dtype, value):
     for part in (x, x[:9].contiguous()):
         codes, scales, _ = binding.spec_norm_fp8(part, gain)
         assert not torch.isfinite(scales).any() and torch.isnan(codes.float() * scales[:, None]).all()
+
+
+@pytest.mark.parametrize("d", WIDTHS)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_squares_past_the_range_are_not_a_row_of_zeros(d, dtype):
+    x, gain = normal(d, 160, d), 1 + 0.1 * normal(d + 1, d)
+    x[1] *= 1e25
+    x[2] *= 1e15      # (squares of 1e30: within it)
+    x[3] = 0
+    x[3, 1] = 2e19
+    x[4] = 0
+    x[4, 1] = 1e19
+    x = x.to(dtype)
+    for rows in (slice(0, 5), slice(None)):
+        codes, scales, _ = binding.spec_norm_fp8(x[rows].contiguous().cuda(), gain.cuda())
+        fine = [0, 2, 4]
+        assert torch.isnan(scales[[1, 3]]).all() and torch.isnan(codes[[1, 3]].float()).all()
+        w = x[fine].double()
+        rows8.check_codes(codes[fine], scales[fine], w * gain.double() / torch.sqrt((w * w).mean(-1, keepdim=True) + 1e-6), E4M3, NORM_REL)
