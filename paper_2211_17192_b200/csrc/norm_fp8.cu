@@ -24,20 +24,32 @@ __device__ __forceinline__ float larger_magnitude(float m, float v) {
     return m;
 }
 
-// The row's scale, and what its values (before the norm's factor) are multiplied with to be its codes.
-template <bool NORM>
-__device__ __forceinline__ float code_factor(uint32_t largest, float squares, int d, float eps, float& scale) {
-    float factor = 1.0f;
-    uint32_t top = largest;
-    if constexpr (NORM) {
-        // (squares that add up past fp32's range are no mean: a factor of zero would make a row of zeros of the largest there are)
-        factor = squares < INFINITY ? __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(squares, static_cast<float>(d)) + eps)) : NAN;
-        top = magnitude(__uint_as_float(largest) * factor);
+// The row's scale, and what its values (before the norm's factor) are multiplied with to be its codes: first with `lift`, 1 or a power of two
+// where the other alone would be past fp32's range (448 / 10^-36, or 2^48 and more in front of the least scale: not unless eps is
+// below kTinyEps), then with what is returned.
+constexpr float kTinyEps = 0x1p-90f;
+template <bool NORM, bool TINY>
+__device__ __forceinline__ float code_factor(uint32_t largest, float squares, int d, float eps, float& scale, float& lift) {
+    constexpr float kLift = 0x1p64f;
+    lift = 1.0f;
+    if constexpr (!NORM) {
+        scale = row_scale(largest, kE4m3Top);
+        return __fdiv_rn(1.0f, scale);
     }
+    // (squares that add up past fp32's range are no mean: a factor of zero would make a row of zeros of the largest there are)
+    float factor = squares < INFINITY ? __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(squares, static_cast<float>(d)) + eps)) : NAN;
+    const float most = __uint_as_float(largest);
+    const uint32_t top = magnitude(most * factor);
     scale = row_scale(top, kE4m3Top);
-    // a row of zeros, of values that no scale is small enough for, of no numbers, or one that is not normalised
-    if (!NORM || top == 0u || scale == kLeastScale || !(scale < 3.0e38f)) return factor * __fdiv_rn(1.0f, scale);
-    return __fdiv_rn(kE4m3Top, __uint_as_float(largest));
+    if (top == 0u || scale == kLeastScale || !(scale < 3.0e38f)) {  // a row of zeros, of values that no scale is small enough for, of no numbers
+        if (TINY && factor > 0x1p46f) {
+            lift = kLift;
+            factor *= 1.0f / kLift;
+        }
+        return factor * __fdiv_rn(1.0f, scale);
+    }
+    if (TINY && most < 0x1p-118f) lift = kLift;
+    return __fdiv_rn(kE4m3Top, TINY ? most * lift : most);
 }
 
 // Between its two passes a row is held as HOLD, the type it is stored in: as fp32 the registers left one CTA of a 2048 x 11008
@@ -123,8 +135,8 @@ rows_fp8_kernel(const TX* x, const TH* residual, TH* h, const float* __restrict_
         if constexpr (NORM) squares = warp_sum(lane < warps ? part_squares[lane] : 0.0f);
         largest = __reduce_max_sync(kFullMask, lane < warps ? part_largest[lane] : 0u);
     }
-    float scale;
-    const float factor = code_factor<NORM>(largest, squares, d, eps, scale);
+    float scale, lift;
+    const float factor = code_factor<NORM, true>(largest, squares, d, eps, scale, lift);
     if (threadIdx.x == 0) scales[row] = scale;
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) {
@@ -133,7 +145,7 @@ rows_fp8_kernel(const TX* x, const TH* residual, TH* h, const float* __restrict_
         if constexpr (NORM) take(gain, c0, w);
         uint32_t packed[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) packed[i] = codes_e4m3(value(g, w, 2 * i) * factor, value(g, w, 2 * i + 1) * factor);
+        for (int i = 0; i < 4; ++i) packed[i] = codes_e4m3(value(g, w, 2 * i) * lift * factor, value(g, w, 2 * i + 1) * lift * factor);
         if (wide) {
             if (c0 < d) *reinterpret_cast<uint2*>(codes + c0) = make_uint2(packed[0] | packed[1] << 16, packed[2] | packed[3] << 16);
         } else {
@@ -278,8 +290,8 @@ rows_fp8_stream_kernel(const __grid_constant__ RowsArgs a) {
 #pragma unroll
             for (int w = 0; w < kStreamWarps; ++w) squares += part_squares[turn][w];
         }
-        float scale;
-        const float factor = code_factor<NORM>(largest, squares, d, a.eps, scale);
+        float scale, lift;
+        const float factor = code_factor<NORM, false>(largest, squares, d, a.eps, scale, lift);
         if (threadIdx.x == 0) a.scales[row] = scale;
 #pragma unroll
         for (int g = 0; g < ITER; ++g) {
@@ -299,8 +311,8 @@ int launch_rows(RowsArgs a, cudaStream_t stream) {
     a.stage_bytes = a.d * static_cast<int>(sizeof(TX) + (summed ? sizeof(TH) : 0));
     // 2048 x 4096 bf16 with a bf16 residual: 11.5 us here, 16.3 with a CTA to a row; 150 rows 2.5 and 3.5; 2048 x 1024 9.1 and 5.4 (a
     // thread has eight columns of a row, and half of them have none).  Two CTAs to an SM and 48 KB of ring to each: with 64 KB the
-    // next kernel's CTAs find no room beside these before they end (14.2 us).
-    if (a.wide && a.d >= 2048 && a.d <= 16384 && a.rows >= 148 && a.stage_bytes <= 56 * 1024 && (!summed || std::is_same_v<HOLD, TH>)) {
+    // next kernel's CTAs find no room beside these before they end (14.2 us).  (A tiny eps takes one product more for a code: 13.0 for 12.7 us here.)
+    if (a.wide && a.d >= 2048 && a.d <= 16384 && a.rows >= 148 && a.stage_bytes <= 56 * 1024 && (!NORM || a.eps >= kTinyEps) && (!summed || std::is_same_v<HOLD, TH>)) {
         a.stages = std::max(2, std::min(kStreamStages, 48 * 1024 / a.stage_bytes));
         const int smem = a.stages * a.stage_bytes, rounds = (a.rows + 2 * 148 - 1) / (2 * 148);
         const auto go = [&](auto kernel, std::atomic<unsigned long long>& configured) {

@@ -104,3 +104,25 @@ def test_squares_past_the_range_are_not_a_row_of_zeros(d, dtype):
         assert torch.isnan(scales[[1, 3]]).all() and torch.isnan(codes[[1, 3]].float()).all()
         w = x[fine].double()
         rows8.check_codes(codes[fine], scales[fine], w * gain.double() / torch.sqrt((w * w).mean(-1, keepdim=True) + 1e-6), E4M3, NORM_REL)
+
+
+@pytest.mark.parametrize("d", WIDTHS)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size,gain,eps", [(1e-18, 1e-18, 1e-30), (1e-20, 1e-16, 1e-36), (1e-19, 1e-18, 1e-30), (1e-25, 1e-12, 1e-38), (1e-15, 1e-25, 1e-30),
+                                           (1e-18, 1e-17, 2.0 ** -90), (1e-20, 1e-17, 2.0 ** -90)])
+def test_tiny_rows_under_a_tiny_eps(d, dtype, size, gain, eps):
+    # h * gain of about 10^-36: 448 of that is past fp32's range, y itself is not small.  (In the third case y is below 448 of the least
+    # scale, 2^-80.  The last eps is the least that calls of many rows take to the kernel for these.)
+    x = (normal(d, 160, d) * size).to(dtype)
+    x[:, 1::7] = 0
+    x[2] = 0
+    gains = torch.full((d,), gain)
+    for rows in (slice(0, 5), slice(None)):
+        codes, scales, _ = binding.spec_norm_fp8(x[rows].contiguous().cuda(), gains.cuda(), eps)
+        w = x[rows].double()
+        e = torch.tensor(eps, dtype=F32).double()  # (as the kernel is given it)
+        # h * gain is rounded to fp32, among the subnormals too (by 2^-150, which is much of a small element): the same product here.  Squares
+        # and their sums are off by 2^-150 each there, d of them at most, which is in the row's factor.
+        y = (x[rows].float() * gains).double() / torch.sqrt((w * w).mean(-1, keepdim=True) + e)
+        small = float(d * 2.0 ** -150 / ((w * w).mean(-1) + e).min())
+        rows8.check_codes(codes, scales, y, E4M3, NORM_REL + small)
