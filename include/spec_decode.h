@@ -700,7 +700,7 @@ int spec_timeout_drill(void* stream);
  *   with q_out) [batch, rows, n_heads, d_head] of `dtype` with q_stride gets the
  *   same rotation, rounded into q_out (dense; may be q if that is dense); rows
  *   that are left out are not touched, those whose position has no page are
- *   rotated.  fp16 pools hold +-65504 for what is beyond.
+ *   rotated.  fp16 pools hold +-65504 for finite values beyond.
  *
  * spec_kv_read: what lies where an append with the same start, counts and rows (and
  *   no rope) writes, into k and v [batch, rows, n_kv_heads, d_head] of `dtype`; rows

@@ -95,11 +95,14 @@ kv_append_kernel(const T* q, const T* k, const T* v, long long q_stride, long lo
             }
         } else if (write) {
             using E = std::conditional_t<KV == SPEC_DTYPE_BF16, __nv_bfloat16, __half>;
-            if constexpr (KV == SPEC_DTYPE_FP16) {  // (finite values past the type's range are held as its largest, as in the engine's caches)
+            if constexpr (KV == SPEC_DTYPE_FP16) {  // (finite values past the type's range are held as its largest; infinities stay what they are)
+                const auto held = [](float& x) {
+                    if (fabsf(x) > 65504.0f && fabsf(x) < INFINITY) x = copysignf(65504.0f, x);
+                };
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    if (fabsf(lo[i]) > 65504.0f) lo[i] = copysignf(65504.0f, lo[i]);
-                    if (fabsf(hi[i]) > 65504.0f) hi[i] = copysignf(65504.0f, hi[i]);
+                    held(lo[i]);
+                    held(hi[i]);
                 }
             }
             E* out = static_cast<E*>(pool) + at * D + 8 * l;
