@@ -715,15 +715,16 @@ int spec_timeout_drill(void* stream);
  *   and out 8-byte aligned), out dense and of the same type; query head h reads
  *   KV head h / (n_heads / n_kv_heads).  A 16-bit pool has q's type, an 8-bit one
  *   goes with either.  Lengths past the table's capacity: keys beyond do not
- *   exist.  Queries are multiplied in fp16 after a power of two per row (bf16
- *   pools: as they are), weights are rounded to 16 bits for the second product,
- *   all sums are fp32.  workspace: spec_paged_attention_workspace_bytes() bytes,
- *   256-byte aligned, contents arbitrary, not shared by calls that may overlap.
- *   Scales of an 8-bit pool are 16-byte aligned here.  Weights are rounded against the
- *   largest weight times V scale of a row; a V row of zeros with the scale 1, as it is
- *   appended, does not count there.  rows <= 65536, heads of a KV
- *   head <= 1024, rows times these <= 2^20; batch * n_kv_heads * (blocks of 32
- *   queries) * (tiles of 64 keys that the table has room for, and three) <= 2^30.
+ *   exist.  Queries are multiplied as they are, bf16 ones of an 8-bit pool in fp16
+ *   after a power of two per row; weights are rounded for the second product, to
+ *   bf16 over bf16 pools and to fp16 over the others; all sums are fp32.  Over 8-bit
+ *   pools they are rounded against the largest weight times V scale of a row; a V row
+ *   of zeros with the scale 1, as it is appended, does not count there.  workspace:
+ *   spec_paged_attention_workspace_bytes() bytes, 256-byte aligned, contents
+ *   arbitrary, not shared by calls that may overlap.  Scales of an 8-bit pool are
+ *   16-byte aligned here.  rows <= 65536, heads of a KV head <= 1024, rows times
+ *   these <= 2^20; batch * n_kv_heads * (blocks of 32 queries) * (tiles of 64 keys
+ *   that the table has room for, and three) <= 2^30.
  *
  * Errors: SPEC_ERR_BAD_ARG for null pointers, sizes, types, alignments or strides
  * other than described (nothing is launched then); SPEC_ERR_CUDA if a launch fails.

@@ -460,7 +460,8 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
 
         // ---- the block's queries ----
         // Lane c of a quad reads dims E (4 i + c) + 4 s .. + 3 of a key row (E elements to 16 bytes), so step E/4 i + s of the
-        // product takes the same dims of the query.  fp16 rows are brought to a largest magnitude in [1, 2) by a power of two.
+        // product takes the same dims of the query.  bf16 rows for fp16 products are brought to a largest magnitude in [1, 2) by a power
+        // of two; fp16 rows are taken as they are (their small elements would lose bits so).
         constexpr int E = 16 / (S::kRowBytes / D), kPerChunk = E / 4;
         const uint4* q_frag = reinterpret_cast<const uint4*>(queries + turn * S::kQueryBytes);
         const float* q_factor = query_factor + turn * S::kQueries;
@@ -477,7 +478,7 @@ paged_attention_kernel(const __grid_constant__ CUtensorMap map, const __grid_con
                 else load_row(reinterpret_cast<const __half*>(from), true, v);
             }
             float back = 1.0f;
-            if constexpr (!S::kBf16) {
+            if (!S::kBf16 && a.q_bf16) {
                 uint32_t largest = 0u;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) largest = max(largest, magnitude(v[i]));
