@@ -362,6 +362,7 @@ def _operand(t, name, dtypes, shape=None, contiguous=True):
     _need(t.device.index == torch.cuda.current_device(), f"{name} is on {t.device}, not on the current device")
     _need(t.dtype in dtypes, f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
     _need(shape is None or tuple(t.shape) == tuple(shape), f"{name} must be {list(shape) if shape is not None else ''}, got {list(t.shape)}")
+    _need(max(t.shape, default=0) < 2 ** 31, f"{name} is {list(t.shape)}: the library counts in 32 bits")  # (ctypes would pass what is left of the number)
     _need(not contiguous or t.is_contiguous(), f"{name} must be contiguous")
     return t.data_ptr()
 
