@@ -501,7 +501,8 @@ def spec_kv_append(k, v, pool, scales, page_table, start, counts=None, rope=None
     v_at, v_stride = _rows_of_heads(v, "v", (k.dtype,), k.shape)
     n_heads, q_at, q_stride, out = 0, None, 0, None
     if q is not None:
-        _need(q.dim() == 4 and q.shape[0] == batch and q.shape[1] == rows and q.shape[3] == d, "q must be [B, rows, heads, d_head]")
+        _need(isinstance(q, torch.Tensor) and q.dim() == 4 and q.shape[0] == batch and q.shape[1] == rows and q.shape[3] == d,
+              "q must be [B, rows, heads, d_head]")
         n_heads = q.shape[2]
         q_at, q_stride = _rows_of_heads(q, "q", (k.dtype,))
         q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
@@ -509,7 +510,7 @@ def spec_kv_append(k, v, pool, scales, page_table, start, counts=None, rope=None
     else:
         _need(q_out is None, "q_out goes with q")
     if rope is not None:
-        _need(rope.dim() == 3 and tuple(rope.shape[1:]) == (d // 2, 2), "rope must be [positions, d_head / 2, 2]")
+        _need(isinstance(rope, torch.Tensor) and rope.dim() == 3 and tuple(rope.shape[1:]) == (d // 2, 2), "rope must be [positions, d_head / 2, 2]")
     _check(lib().spec_kv_append(q_at, k_at, v_at, _DTYPE_CODES[k.dtype], q_stride, k_stride, v_stride, n_heads, n_kv, d, batch, rows,
                                 _operand(start, "start", (torch.int32,), (batch,)), _optional(counts, "counts", (torch.int32,), (batch,)),
                                 _optional(rope, "rope", (torch.float32,)), 0 if rope is None else rope.shape[0], out, where, at, kv_dtype, pages,
@@ -546,7 +547,7 @@ def spec_paged_attention(q, pool, scales, page_table, lengths, scale=None, out=N
     bf16 or fp16, the cache as in `spec_kv_append`, lengths [B] int32 the tokens cached with the new ones; row i sees the keys at
     and before position lengths[b] - rows + i.  scale defaults to d_head ** -0.5.  Returns out, of q's shape and type; it and
     the workspace are allocated when not given."""
-    if out is not None and workspace is not None and _short(q):
+    if out is not None and workspace is not None and _short(q) and q.dim() == 4 and q.shape[3]:
         device = _device()
         if _made(_calls.attention(q, pool, scales, page_table, lengths, q.shape[-1] ** -0.5 if scale is None else scale, out, workspace, device,
                                   _raw_stream(device))):
@@ -554,7 +555,7 @@ def spec_paged_attention(q, pool, scales, page_table, lengths, scale=None, out=N
     _need(isinstance(q, torch.Tensor) and q.dim() == 4, "q must be [B, rows, heads, d_head]")
     batch, rows, heads, d = q.shape
     where, at, kv_dtype, pages, page_size, table, width, n_kv, pool_d = _pool_args(pool, scales, page_table, batch)
-    _need(d == pool_d and heads % n_kv == 0, "q and the pool differ in d_head, or its heads are no multiple of the pool's")
+    _need(0 < d == pool_d and n_kv > 0 and heads % n_kv == 0, "q and the pool differ in d_head, or its heads are no multiple of the pool's")
     q_at, q_stride = _rows_of_heads(q, "q", (torch.bfloat16, torch.float16))
     out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
     if workspace is None:
