@@ -249,14 +249,13 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
     // The next kernel is let in when this CTA's copies and products have been asked for.  At the top it takes the places of CTAs that
     // leave, an SM here and there, and its own stream is then as uneven (3 x 4096 x 22016, call after call: 18.7 us, 16.8 so).
     if (warp < 2) pdl_trigger();
-    // (a CTA without a k-block has nothing to wait for and adds nothing)
     const int quarter = warp & 3;  // accumulator lanes 32 quarter .. + 31 are what warps 2..5 may read
-    const bool reader = warp >= 2, have = kb1 > kb0;
+    const bool reader = warp >= 2;  // (of sums: every CTA has a k-block, launch_small)
     const int valid = min(a.tokens, a.rows - row0);
     LaneColumn column{};
     if (reader) {
         column = lane_column(a, tile, quarter, lane);
-        if (have && !mbar_wait_warp(acc_bar, 0, a.limit)) ok = false;
+        if (!mbar_wait_warp(acc_bar, 0, a.limit)) ok = false;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     }
     const uint32_t acc = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
@@ -277,12 +276,8 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_consta
         if (reader && ok)
             for (int c0 = 0; c0 < valid; c0 += 16) {
                 uint32_t v[16];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] = 0u;
-                if (have) {
-                    tmem_ld16(acc + c0, v);
-                    tmem_ld_wait();
-                }
+                tmem_ld16(acc + c0, v);
+                tmem_ld_wait();
                 int to = c0 / each, within = c0 - to * each;
 #pragma unroll
                 for (int i = 0; i < 16; i += 4)
@@ -543,7 +538,7 @@ int launch_small(const void* x, const void* w, int k, LinearArgs a, cudaStream_t
     const bool paired = a.tokens <= 64;
     int splits = 1;
     for (int s = 2; s <= (paired ? 8 : 4); ++s)
-        if (tiles * token_tiles * s <= (paired ? 200 : 128) && 2 * s <= a.k_blocks) splits = s;
+        if (tiles * token_tiles * s <= (paired ? 200 : 128) && 2 * s <= a.k_blocks) splits = s;  // (two k-blocks to a CTA at least)
     const int stage_bytes = kTileBytes + a.tokens * kBlockK, exchange = exchange_bytes(a.tokens, splits);
     const int room = (paired ? 113 : 227) * 1024 - 1024 - 512 - exchange;
     a.stages = std::min({kMaxStages, room / stage_bytes, std::max(2, (a.k_blocks + splits - 1) / splits)});

@@ -59,7 +59,7 @@ struct AttnArgs {
     float2* partial_ml;  // [CTA][2][queries of a block]: maximum, sum
     long long q_stride;
     float scale;
-    int batch, rows, n_heads, group, blocks, units;  // blocks: of queries per (sequence, KV head); units = batch * blocks
+    int rows, n_heads, group, blocks, units;  // blocks: of queries per (sequence, KV head); units = batch * blocks
     int q_bf16, q_wide /* q's rows start on 16 bytes */, grid;
     uint32_t by_group;  // ceil(2^32 / group) for groups of two and more
     // The token of a query of a (sequence, KV head); exact, since query * group stays below 2^31.
@@ -1077,7 +1077,6 @@ extern "C" int spec_paged_attention(const void* q, int dtype, int64_t q_stride, 
     a.partial_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + align256(slots * queries * d_head * 4));
     a.q_stride = q_stride;
     a.scale = scale;
-    a.batch = batch;
     a.rows = rows;
     a.n_heads = n_heads;
     a.units = static_cast<int>(units);
