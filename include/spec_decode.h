@@ -620,11 +620,12 @@ int spec_device_error(void);
  * The codes are per device, not per context: whichever context synchronises next reports a time-out
  * of another's kernel on the same device.  These calls exercise the path without breaking anything.
  *
- * spec_timeout_drill launches the two tensor-core GEMM kernels (one CTA, and a CTA pair) on one
- * tile each with their producers switched off (nothing is requested from memory, so nothing is in
- * flight when the CTAs give up) and a limit of 4096 polls, waits for them, and returns
- * SPEC_ERR_DEVICE_TIMEOUT if both reported the expired wait as they should (SPEC_ERR_CUDA if not).
- * The device error flags are clear afterwards and the context stays usable.  Synchronises `stream`.
+ * spec_timeout_drill launches the two tensor-core GEMM kernels (one CTA, and a CTA pair) and the two of
+ * spec_linear_fp8 (a cluster of two, and a CTA pair) on one tile each with their producers switched off
+ * (nothing is requested from memory, so nothing is in flight when the CTAs give up) and a limit of 4096
+ * polls, waits for them, and returns SPEC_ERR_DEVICE_TIMEOUT if all reported the expired wait as they
+ * should (SPEC_ERR_CUDA if not).  The device error flags are clear afterwards and the context stays
+ * usable.  Synchronises `stream`.
  *
  * spec_timeout_drill_pass does the same for the kernel that runs few-row passes of a small bf16 model
  * (which: 0 target, 1 draft) as one grid, or of a tiny fp32 one as one cluster: a row at the cached length of sequence 0, of which no CTA

@@ -638,7 +638,7 @@ extern "C" int spec_pack_weight(const void* w, int n_out, int k, void* packed, v
 
 // ---- C ABI: a bounded wait that runs out, on purpose ----
 namespace {
-__device__ __align__(1024) unsigned char g_drill_tile[128 * 64 * 2];  // what the drill's tensor maps point at (never read)
+__device__ __align__(1024) unsigned char g_drill_tile[128 * 64 * 2];  // what the drill's tensor maps point at (of which some zeros are read as scales)
 }
 
 extern "C" int spec_timeout_drill(void* stream) {
@@ -661,9 +661,18 @@ extern "C" int spec_timeout_drill(void* stream) {
     if (status != SPEC_OK) return status;
     SPEC_CUDA_TRY(cudaStreamSynchronize(st));
     const int code = gemm_tc_take_error(), wide = gemm_wide_take_error();
-    if (code > 0 && wide > 0)
-        return fail(SPEC_ERR_DEVICE_TIMEOUT, "drill: the kernels gave up on a bounded wait (codes %d, %d), freed their tensor memory and returned", code, wide);
-    return fail(SPEC_ERR_CUDA, "drill: a kernel did not report the wait that should have run out (codes %d, %d)", code, wide);
+    // the same with the kernels of spec_linear_fp8, one after the other: they share their word
+    int linear[2];
+    linear_fp8_take_error();
+    for (int i = 0; i < 2; ++i) {
+        status = launch_linear_fp8_drill(base, i == 1, 4096, st);
+        if (status != SPEC_OK) return status;
+        SPEC_CUDA_TRY(cudaStreamSynchronize(st));
+        linear[i] = linear_fp8_take_error();
+    }
+    if (code > 0 && wide > 0 && linear[0] > 0 && linear[1] > 0)
+        return fail(SPEC_ERR_DEVICE_TIMEOUT, "drill: the kernels gave up on a bounded wait (codes %d, %d, %d, %d), freed their tensor memory and returned", code, wide, linear[0], linear[1]);
+    return fail(SPEC_ERR_CUDA, "drill: a kernel did not report the wait that should have run out (codes %d, %d, %d, %d)", code, wide, linear[0], linear[1]);
 }
 
 extern "C" int spec_device_error(void) {

@@ -139,6 +139,7 @@ int launch_gemm_wide(const __nv_bfloat16* hi, const __nv_bfloat16* lo, int hi_ro
                      int n_out, int k, float* partial, bool fill, cudaStream_t stream);
 int gemm_wide_take_error();
 int linear_fp8_take_error();       // linear_fp8.cu
+int launch_linear_fp8_drill(void* base, bool wide, uint32_t limit, cudaStream_t stream);
 int paged_attention_take_error();  // paged_attention.cu
 int norm_fp8_take_error();         // norm_fp8.cu
 int launch_gemm_wide_drill(void* base, uint32_t limit, cudaStream_t stream);
