@@ -126,3 +126,19 @@ def test_tiny_rows_under_a_tiny_eps(d, dtype, size, gain, eps):
         y = (x[rows].float() * gains).double() / torch.sqrt((w * w).mean(-1, keepdim=True) + e)
         small = float(d * 2.0 ** -150 / ((w * w).mean(-1) + e).min())
         rows8.check_codes(codes, scales, y, E4M3, NORM_REL + small)
+
+
+@pytest.mark.parametrize("rows,d", [(5, 768), (3, 4104), (300, 2048), (200, 4096), (160, 11003)])
+@pytest.mark.parametrize("dtype,h_dtype", [(F32, F32), (BF16, BF16), (BF16, F32), (F16, F16), (F16, F32)])
+def test_a_sum_that_is_not_stored(rows, d, dtype, h_dtype):
+    # the library's form without h: the sum is not rounded to h's type on its way (16-bit sums are of two 16-bit values: exact in fp32 or
+    # off by 2^-24)
+    kinds = {F32: 0, BF16: 1, F16: 2}
+    x, residual, gain = normal(d, rows, d).to(dtype).cuda(), (normal(d + 1, rows, d) * 5).to(h_dtype).cuda(), (1 + 0.1 * normal(d + 2, d)).cuda()
+    kept = residual.clone()
+    codes, scales = torch.empty(rows, d, dtype=E4M3, device="cuda"), torch.empty(rows, device="cuda")
+    assert binding.lib().spec_norm_fp8(x.data_ptr(), kinds[dtype], residual.data_ptr(), None, kinds[h_dtype], gain.data_ptr(), 1e-6, rows, d,
+                                       codes.data_ptr(), scales.data_ptr(), torch.cuda.current_stream().cuda_stream) == 0
+    w = (x.float() + residual.float()).double()
+    rows8.check_codes(codes, scales, w * gain.double() / torch.sqrt((w * w).mean(-1, keepdim=True) + 1e-6), E4M3, NORM_REL)
+    assert torch.equal(residual, kept)
