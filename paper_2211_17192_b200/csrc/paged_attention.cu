@@ -39,10 +39,11 @@ constexpr int most_ctas(int queries) { return 148 * (queries == 8 ? 5 : queries 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kSwitch = 3;       // tiles that taking up another segment costs about as much as
 constexpr float kNone = -3.0e38f;  // the running maximum where no key has been seen: finite, so that differences stay numbers
-// What a V row of zeros is taken to have for a scale: the least there is, for the 1 that it is stored with, which says nothing and would let
-// such a row set the maximum (beside a sink of zeros that led by ten, rows with scales of 2^-12 had weights among fp16's subnormals:
-// outputs off by 7 %).
-constexpr float kScaleOfZeros = kLeastScale;
+// What a V row of zeros is taken to have for a scale, for the 1 that it is stored with, which says nothing and would let such a row set the
+// maximum (beside a sink of zeros that led by ten, rows with scales of 2^-12 had weights among fp16's subnormals: outputs off by 7 %).
+// Small, so that a row whose scale is s loses nothing to one that leads by 2^(78 + log2 s), and not smaller, since weights below 2^-126
+// of the largest are none: beside rows of a scale s, zeros with 2^(log2 s - 62) of their weight and less leave the sum.
+constexpr float kScaleOfZeros = 0x1p-64f;
 constexpr float kSlack = 8.0f;   // the running maximum may lag by this: w <= 2^8 stays in fp16's range
 
 __device__ int g_paged_error;  // set when the bounded wait for a tile or for its place ran out (0 = none)

@@ -70,3 +70,20 @@ def test_rows_of_zeros_alone_give_zeros(kind, rows):
     got = binding.spec_paged_attention(q, pool, scales, table, at)
     want, bound = rows8.attention64(q, pool, scales, table, at, 64 ** -0.5)
     assert want[0].any() and torch.all((got.cpu().double() - want).abs() <= (bound - 2.0 ** -25).clamp_min(0))
+
+
+@pytest.mark.parametrize("kind", [E4M3, INT8])
+@pytest.mark.parametrize("rows", [2, 12])
+def test_rows_of_zeros_count_beside_large_ones(kind, rows):
+    # half of the rows are zeros, of a weight of e^-10 each: together a few per cent of the sum, whatever the others' sizes
+    batch, width, size = 2, 12, 64
+    pool, scales, table = cache_with_zero_rows(2, kind, 1, 64, size, batch, width, list(range(1, width * size, 2)), 1e12, -10.0)
+    rng = np.random.default_rng(9)
+    q = 0.1 * torch.from_numpy(rng.standard_normal((batch, rows, 4, 64), dtype=np.float32))
+    q[..., 0] = 1.0
+    q = q.to(BF16).cuda()
+    pool.view(torch.uint8)[:, 0, :, 0::2] = 0  # (keys without a score)
+    at = torch.tensor([768, 200], dtype=torch.int32, device="cuda")
+    got = binding.spec_paged_attention(q, pool, scales, table, at, scale=1.0)
+    want, bound = rows8.attention64(q, pool, scales, table, at, 1.0)
+    assert torch.all((got.cpu().double() - want).abs() <= bound)
