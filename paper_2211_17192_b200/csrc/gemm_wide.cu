@@ -360,7 +360,12 @@ int launch_gemm_wide_drill(void* base, uint32_t limit, cudaStream_t stream) {
     int status = cached_bf16_map(base, kTileM, kTileK, kTileM, true, &mw);
     if (status == SPEC_OK) status = cached_bf16_map(base, 16, kTileK, 16, true, &mx);
     if (status != SPEC_OK) return status;
-    const int smem = a.stages * (kWeightBytes + a.sub_rows * kTileK * 2) + 1024 + 512;
+    // (as much shared memory as a real launch: nothing with tensor memory of its own then lies beside these CTAs, which take all of it and wait
+    // for each other; a pair that waits for columns of another stream's cluster, which waits for the pair's, would wait for ever)
+    const int smem = kSmemBudget + 1024 + 512;
+    static std::atomic<unsigned long long> configured{0};
+    status = allow_shared_memory(configured, gemm_wide_kernel, 227 * 1024);
+    if (status != SPEC_OK) return status;
     return launch_pdl(gemm_wide_kernel, dim3(2 * a.plan.pairs), dim3(kWideThreads), smem, stream, mw, mx, mx, static_cast<float*>(base), a);
 }
 

@@ -27,3 +27,22 @@ def test_waits_that_run_out_are_reported_and_leave_the_kernels_usable():
         for x, y in zip(xs, want):
             assert torch.equal(binding.spec_linear_fp8(*x, *w), y)
     assert binding.spec_device_error() == 0
+
+
+def test_a_drill_beside_clusters_of_another_stream():
+    # the drills' CTAs and those of the layer's clusters all take tensor memory, and wait for CTAs on other SMs
+    h = binding.lib()
+    h.spec_timeout_drill.restype = ctypes.c_int
+    h.spec_timeout_drill.argtypes = [ctypes.c_void_p]
+    g = torch.Generator(device="cuda").manual_seed(2)
+    w = binding.spec_quantize_fp8(torch.randn(4096, 4096, device="cuda", generator=g))
+    x = binding.spec_quantize_fp8(torch.randn(5, 4096, device="cuda", generator=g))
+    want = binding.spec_linear_fp8(*x, *w)
+    side, got = torch.cuda.Stream(), []
+    torch.cuda.synchronize()
+    for _ in range(5):
+        with torch.cuda.stream(side):
+            got += [binding.spec_linear_fp8(*x, *w) for _ in range(40)]
+        assert h.spec_timeout_drill(torch.cuda.current_stream().cuda_stream) == -6, h.spec_last_error().decode()
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want) for y in got) and binding.spec_device_error() == 0
