@@ -658,7 +658,8 @@ int spec_timeout_drill(void* stream);
  *
  * spec_quantize_fp8: x [rows, d] fp32, bf16 or fp16 (x_dtype) to e4m3 codes
  *   [rows, d] and scales [rows]; 1 <= d <= 32768.  Also makes the weights of
- *   spec_linear_fp8 (a scale per row of W).
+ *   spec_linear_fp8 (a scale per row of W) for k up to that; longer rows of codes and
+ *   their scales are made elsewhere.
  *
  * spec_norm_fp8: h = x + residual, rounded to h_dtype (fp32 or x's) where it is
  *   stored; y = (h * gain) * (mean(h^2) + eps)^(-1/2) over the row; codes and

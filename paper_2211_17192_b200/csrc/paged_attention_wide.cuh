@@ -9,8 +9,8 @@
 // tiles, one that issues the products, and two that only make up the last one's four, since registers are shared out among fours.
 // S has two places: K of tile j + 1 is multiplied while the weights of tile j are made; two CTAs share an SM and its 512 columns.
 // What bounds it: the chain weights -> second product -> free place -> widened K -> first product of every other tile, and the
-// exponentials (1024 of a tile's 3000 cycles); 32 heads over 8 of 128 dims, 512 rows over 8192 tokens: 405 TFLOP/s int8; one prompt of
-// 4096 rows 408 us.  (Queries fetched by the widening warps, with shuffles for their maxima: two prompts of 1024 rows 161 us, so 105;
+// exponentials (1024 of a tile's 3000 cycles); 32 heads over 8 of 128 dims, 512 rows over 8192 tokens: 403 TFLOP/s int8; one prompt of
+// 4096 rows 416 us.  (Queries fetched by the widening warps, with shuffles for their maxima: two prompts of 1024 rows 161 us, so 105;
 // eight widening warps, K beside V: no faster; the widening loop rolled up instead of its loads in flight together: 77 us for 75.)
 #pragma once
 
