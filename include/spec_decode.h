@@ -684,7 +684,8 @@ int spec_timeout_drill(void* stream);
  * Paged K,V rows: pool [pages][K, V][n_kv_heads][page_size][d_head] in kv_dtype
  * (SPEC_DTYPE_FP16, BF16, E4M3 or INT8), 16-byte aligned, and for the two 8-bit
  * types scales [pages][K, V][n_kv_heads][page_size] fp32 (a scale per token and
- * head; those of rows that are read have to be above zero).  page_size: a power
+ * head; those of rows that are read lie in 2^-126 .. 2^126, as appended ones do, or
+ * are no number, like their rows).  page_size: a power
  * of two from 32 to 256; d_head 64 or 128.  page_table [batch][max_pages] int32:
  * the page of each page_size positions of a sequence, below 2^31 - 256 positions;
  * batch <= 65535, n_kv_heads <= 1024.  An entry outside [0, pages)
